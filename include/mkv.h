@@ -356,6 +356,136 @@ mkv_status mkv_attention_tiles(mkv_cache *cache, int32_t *n_tiles, int32_t *n_ti
 mkv_status mkv_probe_read_bandwidth(const void *buf, size_t bytes, uint32_t *sink, int32_t reps,
                                     double *gbs, void *stream);
 
+/*
+ * Rotary positions, for the queries and keys that the calls above take as rotated.  Each row (a
+ * token) has one position per axis: one axis for text; time, height and width for images and video.
+ * Frequency pair i of a head turns by the angle pos[axis(i)][row] * inv_freq[i], the first
+ * sections[0] pairs by axis 0, the next sections[1] by axis 1, and so on:
+ *   (a, b) -> (a cos - b sin, b cos + a sin)
+ * with (a, b) the values at (i, i + rotary_dim / 2) (MKV_ROPE_HALVES) or (2 i, 2 i + 1)
+ * (MKV_ROPE_PAIRS).  Values from rotary_dim on are copied.  inverse != 0 turns back by the same
+ * angles, which is also the gradient with respect to the unrotated rows.  Angles are formed in 64
+ * bits and reduced before their sine and cosine, so far positions lose nothing; the result is
+ * rounded to fp16 once.
+ *   inv_freq  device float32 [rotary_dim / 2]
+ *   pos       device int32 [n_axes][n_rows]
+ *   sets      host array of 1..MKV_ROPE_MAX_SETS tensors over the same rows (a token's queries and
+ *             its keys): x device fp16, head j of row r at x + r * x_stride + j * head_dim (strides
+ *             in elements), y likewise.  y may be x with the
+ *             same stride (in place); otherwise no output may overlap an input or another output.
+ * n_rows = 0 is accepted and enqueues nothing.  One launch; may be captured.
+ */
+#define MKV_ROPE_MAX_AXES 4
+#define MKV_ROPE_MAX_SETS 4
+typedef enum { MKV_ROPE_HALVES = 0, MKV_ROPE_PAIRS = 1 } mkv_rope_layout;
+
+typedef struct {
+  int32_t head_dim;    /* 2..1024, even */
+  int32_t rotary_dim;  /* 2..head_dim, even */
+  int32_t n_axes;      /* 1..MKV_ROPE_MAX_AXES */
+  int32_t sections[MKV_ROPE_MAX_AXES];  /* pairs per axis, >= 0, summing to rotary_dim / 2 */
+  int32_t layout;      /* mkv_rope_layout */
+} mkv_rope_spec;
+
+typedef struct {
+  const uint16_t *x;
+  uint16_t *y;
+  int64_t x_stride, y_stride;  /* elements from one row to the next, >= n_heads * head_dim */
+  int32_t n_heads;             /* >= 1 */
+} mkv_rope_set;
+
+mkv_status mkv_rope(const mkv_rope_spec *spec, const float *inv_freq, const int32_t *pos, int32_t n_rows,
+                    const mkv_rope_set *sets, int32_t n_sets, int32_t inverse, void *stream);
+
+/*
+ * Drafted trees over a cache: several candidate tokens per sequence attended in one pass, and those
+ * accepted put into the cache.  A drafted node attends to every token that its sequence's cache
+ * holds (their dequantized values, as in mkv_decode_attention) and to the nodes of its own tree that
+ * its mask names, itself among them where its bit is set; drafted keys and values enter the
+ * attention in fp16 and are quantized only when they are accepted.
+ *
+ * For caches of FP16, UQ and KVQ sequences.  H2O and ROCKET sequences make MKV_EUNSUPPORTED: what
+ * their decode step attends to depends on the step before (eviction) or on its own query (top-k), so
+ * one pass over a tree would not be what its tokens' own decode steps compute.
+ *
+ *   q          device fp16 [S][n_nodes][Hq][d]
+ *   k, v       device fp16 [S][n_nodes][Hkv][d]
+ *   mask       device uint64 [S][n_nodes]: bit j of a node's word = it attends to node j (bits of
+ *              nodes that do not exist are ignored; a word of 0 leaves the cached tokens)
+ *   n_valid    optional device int32 [S]: sequence s has only its first n_valid[s] nodes (clamped to
+ *              0..n_nodes); the others are not read and their rows of `out` stay as they were
+ *   out        device fp16 [S][n_nodes][Hq][d]; sums and softmax in 32 bits, rounded once
+ *   workspace  device, >= mkv_tree_workspace(cache, n_nodes) bytes, 256-byte aligned, used until the
+ *              call's work is done: calls that may overlap need one each.  NULL if 0 bytes are needed.
+ * n_nodes is 1..MKV_TREE_MAX_NODES.  After prefill or a completed decode step; changes no state of
+ * the cache.  One launch or two; may be captured (counts are read on the device).
+ */
+#define MKV_TREE_MAX_NODES 64
+
+mkv_status mkv_tree_workspace(mkv_cache *cache, int32_t n_nodes, size_t *bytes);
+mkv_status mkv_tree_attention(mkv_cache *cache, const uint16_t *q, const uint16_t *k, const uint16_t *v,
+                              const uint64_t *mask, const int32_t *n_valid, int32_t n_nodes, uint16_t *out,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Accept drafted tokens: append the keys and values of the nodes path[s][0], path[s][1], ...,
+ * path[s][n_path[s] - 1] to sequence s in this order, each as a decode step's append would
+ * (quantized on the way in).
+ *   k, v    device fp16 [S][n_nodes][Hkv][d], as for mkv_tree_attention
+ *   path    device int32 [S][max_path]; an entry outside 0..n_nodes-1 ends the sequence's path
+ *   n_path  device int32 [S], clamped to 0..max_path; 0 accepts nothing
+ *   counts  optional device int32 [S]: the tokens that each sequence then holds (its kv heads hold
+ *           the same tokens)
+ * The same caches and call order as mkv_tree_attention; max_path >= 1.  How many tokens were
+ * accepted is known to the device alone, so capacity is checked there as for replayed steps: a token
+ * that finds its region full is dropped, and mkv_decode_step's own count of steps does not move.
+ * One launch; may be captured.
+ */
+mkv_status mkv_tree_accept(mkv_cache *cache, const uint16_t *k, const uint16_t *v, int32_t n_nodes,
+                           const int32_t *path, const int32_t *n_path, int32_t max_path, int32_t *counts,
+                           void *stream);
+
+/*
+ * Beam search, selection: the n_select best continuations of each request's beams.  Continuation
+ * (w, t) of beam w by token t has the score
+ *   scores[b][w] + logits[b][w][t] - log sum_u exp(logits[b][w][u])
+ * and a finished beam has one continuation, (w, pad_token), with its score unchanged.  Scores are
+ * formed and compared in 64 bits (the exponentials under the logarithm in 32, their sum in 64); ties
+ * go to the lower w * vocab + t.  A NaN logit counts as -infinity, and a continuation whose score is
+ * not above -infinity (a dead beam's, a banned token's, or NaN) is never chosen: where fewer than
+ * n_select are left, the last outputs are (parent 0, pad_token) with the score -infinity.
+ *   logits     device float32 (MKV_F32) or fp16 (MKV_F16) [n_batch * n_beams] rows of `vocab` values,
+ *              row r at logits + r * row_stride (elements, >= vocab)
+ *   scores     device float32 [n_batch][n_beams]
+ *   finished   optional device uint8 [n_batch][n_beams], nonzero = finished
+ *   token, parent, score_out  device int32, int32, float32 [n_batch][n_select], best first; parent
+ *              is the beam within its request, as mkv_cache_reorder takes it
+ *   workspace  device, >= mkv_beam_workspace() bytes, 256-byte aligned (see mkv_tree_attention)
+ * n_beams 1..MKV_BEAM_MAX, n_select 1..min(2 * MKV_BEAM_MAX, vocab), pad_token 0..vocab-1.  Two launches; may be
+ * captured.  n_batch = 0 is accepted and enqueues nothing.
+ */
+#define MKV_BEAM_MAX 32
+typedef enum { MKV_F32 = 0, MKV_F16 = 1 } mkv_dtype;
+
+mkv_status mkv_beam_workspace(int32_t n_batch, int32_t n_beams, int32_t vocab, int32_t n_select, size_t *bytes);
+mkv_status mkv_beam_select(const void *logits, int32_t dtype, int64_t row_stride, int32_t n_batch, int32_t n_beams,
+                           int32_t vocab, const float *scores, const uint8_t *finished, int32_t pad_token,
+                           int32_t n_select, int32_t *token, int32_t *parent, float *score_out, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
+/*
+ * Beam search, states: the cache's sequences are groups of `width` beams (sequence g * width + w is
+ * beam w of request g), and every beam takes the state that beam parent[g * width + w] of its group
+ * had before the call, in place: the tokens past the prompt (the retained set for H2O), their codes,
+ * scales, outliers, scores and positions, and the counts.  The beams of a group must have the same
+ * configuration and prompt length (MKV_EINVAL otherwise) and must have been given the same prompt:
+ * what the prompt left and decode steps never change is not copied.
+ *   parent  device int32 [S], 0..width-1 within the group; any other value keeps the beam as it is
+ * width 1..MKV_BEAM_MAX, n_seqs a multiple of it.  After prefill or a completed decode step.  One
+ * launch or two; may be captured.
+ */
+mkv_status mkv_cache_reorder(mkv_cache *cache, const int32_t *parent, int32_t width, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -36,6 +36,21 @@ class mkv_shape(ctypes.Structure):
                                               "max_new_tokens")]
 
 
+ROPE_MAX_AXES, ROPE_MAX_SETS, TREE_MAX_NODES, BEAM_MAX = 4, 4, 64, 32
+ROPE_LAYOUTS = {"halves": 0, "pairs": 1}
+F32, F16 = 0, 1
+
+
+class mkv_rope_spec(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("sections", ctypes.c_int32 * ROPE_MAX_AXES), ("layout", ctypes.c_int32)]
+
+
+class mkv_rope_set(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("x_stride", ctypes.c_int64),
+                ("y_stride", ctypes.c_int64), ("n_heads", ctypes.c_int32)]
+
+
 class MkvError(RuntimeError):
     def __init__(self, status, text):
         super().__init__(f"mkv status {status}: {text}")
@@ -71,6 +86,13 @@ _SIGS = {
                                ctypes.POINTER(_I), ctypes.POINTER(_I)]),
     "mkv_kv_memory": (_I, [ctypes.POINTER(mkv_shape), ctypes.POINTER(mkv_config), _I, _I,
                            ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(ctypes.c_size_t)]),
+    "mkv_rope": (_I, [ctypes.POINTER(mkv_rope_spec), _P, _P, _I, ctypes.POINTER(mkv_rope_set), _I, _I, _P]),
+    "mkv_tree_workspace": (_I, [_P, _I, ctypes.POINTER(ctypes.c_size_t)]),
+    "mkv_tree_attention": (_I, [_P, _P, _P, _P, _P, _P, _I, _P, _P, ctypes.c_size_t, _P]),
+    "mkv_tree_accept": (_I, [_P, _P, _P, _I, _P, _P, _I, _P, _P]),
+    "mkv_beam_workspace": (_I, [_I, _I, _I, _I, ctypes.POINTER(ctypes.c_size_t)]),
+    "mkv_beam_select": (_I, [_P, _I, ctypes.c_int64, _I, _I, _I, _P, _P, _I, _I, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "mkv_cache_reorder": (_I, [_P, _P, _I, _P]),
     "mkv_probe_read_bandwidth": (_I, [_P, ctypes.c_size_t, _P, _I, ctypes.POINTER(ctypes.c_double), _P]),
 }
 SYMBOLS = tuple(_SIGS)
@@ -237,3 +259,43 @@ def mkv_attention_tiles(h):
     n, n_uq, n_rk = _I(), _I(), _I()
     _check(lib().mkv_attention_tiles(h, ctypes.byref(n), ctypes.byref(n_uq), ctypes.byref(n_rk)))
     return n.value, n_uq.value, n_rk.value
+
+
+def mkv_rope(head_dim, rotary_dim, sections, layout, inv_freq_ptr, pos_ptr, n_rows, sets, inverse, stream):
+    """sets: sequence of (x pointer, y pointer, x row stride, y row stride, heads), strides in elements."""
+    spec = mkv_rope_spec(head_dim, rotary_dim, len(sections), (_I * ROPE_MAX_AXES)(*sections[:ROPE_MAX_AXES]),
+                         ROPE_LAYOUTS.get(layout, layout))
+    arr = (mkv_rope_set * len(sets))(*sets)
+    _check(lib().mkv_rope(ctypes.byref(spec), inv_freq_ptr, pos_ptr, n_rows, arr, len(sets), int(inverse), stream))
+
+
+def mkv_tree_workspace(h, n_nodes):
+    n = ctypes.c_size_t()
+    _check(lib().mkv_tree_workspace(h, n_nodes, ctypes.byref(n)))
+    return n.value
+
+
+def mkv_tree_attention(h, q_ptr, k_ptr, v_ptr, mask_ptr, n_valid_ptr, n_nodes, out_ptr, ws_ptr, ws_bytes, stream):
+    _check(lib().mkv_tree_attention(h, q_ptr, k_ptr, v_ptr, mask_ptr, n_valid_ptr or None, n_nodes, out_ptr,
+                                    ws_ptr or None, ws_bytes, stream))
+
+
+def mkv_tree_accept(h, k_ptr, v_ptr, n_nodes, path_ptr, n_path_ptr, max_path, counts_ptr, stream):
+    _check(lib().mkv_tree_accept(h, k_ptr, v_ptr, n_nodes, path_ptr, n_path_ptr, max_path, counts_ptr or None, stream))
+
+
+def mkv_beam_workspace(n_batch, n_beams, vocab, n_select):
+    n = ctypes.c_size_t()
+    _check(lib().mkv_beam_workspace(n_batch, n_beams, vocab, n_select, ctypes.byref(n)))
+    return n.value
+
+
+def mkv_beam_select(logits_ptr, dtype, row_stride, n_batch, n_beams, vocab, scores_ptr, finished_ptr, pad_token,
+                    n_select, token_ptr, parent_ptr, score_ptr, ws_ptr, ws_bytes, stream):
+    _check(lib().mkv_beam_select(logits_ptr, dtype, row_stride, n_batch, n_beams, vocab, scores_ptr,
+                                 finished_ptr or None, pad_token, n_select, token_ptr, parent_ptr, score_ptr,
+                                 ws_ptr or None, ws_bytes, stream))
+
+
+def mkv_cache_reorder(h, parent_ptr, width, stream):
+    _check(lib().mkv_cache_reorder(h, parent_ptr, width, stream))

@@ -13,7 +13,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmkv.so")
 
-SOURCES = ["mkv_api.cpp", "calib.cpp", "select.cpp", "k_attn.hip", "k_append.hip", "k_select.hip", "k_probe.hip"]
+SOURCES = ["mkv_api.cpp", "calib.cpp", "select.cpp", "decoding.cpp", "k_attn.hip", "k_append.hip", "k_select.hip", "k_probe.hip",
+           "k_rope.hip", "k_tree.hip", "k_beam.hip", "k_reorder.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -12,6 +12,13 @@ def _ptr(t):
     return 0 if t is None else int(t.data_ptr())
 
 
+def check_tensor(name, t, device, dtype, shape):
+    """A call that reads a device buffer by its pointer needs it to be what the kernels take it for."""
+    if t.device != device or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {device} "
+                         f"(got {t.dtype}, {tuple(t.shape)} on {t.device})")
+
+
 class KVCache:
     """One mixed-configuration KV cache (one attention layer's worth).
 
@@ -80,6 +87,56 @@ class KVCache:
 
     def step(self, k, v, q, out):
         L.mkv_decode_step(self.h, _ptr(k), _ptr(v), _ptr(q), _ptr(out), self.s)
+
+    # ---- drafted trees (mkv_tree_attention, mkv_tree_accept) ----------------------------------
+    def tree_workspace(self, n_nodes):
+        """A workspace of tree_attention for n_nodes nodes, for calls that may overlap or be captured."""
+        # (torch aligns an allocation to 512 bytes)
+        return self.torch.empty(L.mkv_tree_workspace(self.h, n_nodes), dtype=self.torch.uint8, device=self.arena.device)
+
+    def tree_attention(self, q, k, v, mask, out=None, n_valid=None, workspace=None):
+        """Attention of drafted nodes over the cache and each other -> out [S][N][Hq][D] fp16.
+
+        q [S][N][Hq][D], k, v [S][N][Hkv][D] fp16; mask [S][N] int64, bit j of a node's word = it
+        attends to node j; n_valid: optional int32 [S], the nodes each sequence has.  The default
+        workspace is allocated for the call, on the cache's stream."""
+        torch, dev = self.torch, self.arena.device
+        n = q.shape[1] if q.dim() == 4 else 0
+        check_tensor("q", q, dev, torch.float16, (self.S, n, self.Hq, self.D))
+        check_tensor("k", k, dev, torch.float16, (self.S, n, self.Hkv, self.D))
+        check_tensor("v", v, dev, torch.float16, (self.S, n, self.Hkv, self.D))
+        check_tensor("mask", mask, dev, torch.int64, (self.S, n))
+        if n_valid is not None:
+            check_tensor("n_valid", n_valid, dev, torch.int32, (self.S,))
+        with torch.cuda.stream(self.stream):
+            if out is None:
+                out = torch.empty_like(q)
+            else:
+                check_tensor("out", out, dev, torch.float16, (self.S, n, self.Hq, self.D))
+            ws = workspace if workspace is not None else self.tree_workspace(n)
+            L.mkv_tree_attention(self.h, _ptr(q), _ptr(k), _ptr(v), _ptr(mask), _ptr(n_valid), n, _ptr(out), _ptr(ws),
+                                 ws.numel(), self.s)
+        return out
+
+    def tree_accept(self, k, v, path, n_path, counts=None):
+        """Append nodes path[s][:n_path[s]] of k, v [S][N][Hkv][D] to each sequence; path [S][M], n_path [S]
+        int32; counts: optional int32 [S], receives the tokens each sequence then holds."""
+        torch, dev = self.torch, self.arena.device
+        n = k.shape[1] if k.dim() == 4 else 0
+        m = path.shape[1] if path.dim() == 2 else 0
+        check_tensor("k", k, dev, torch.float16, (self.S, n, self.Hkv, self.D))
+        check_tensor("v", v, dev, torch.float16, (self.S, n, self.Hkv, self.D))
+        check_tensor("path", path, dev, torch.int32, (self.S, m))
+        check_tensor("n_path", n_path, dev, torch.int32, (self.S,))
+        if counts is not None:
+            check_tensor("counts", counts, dev, torch.int32, (self.S,))
+        L.mkv_tree_accept(self.h, _ptr(k), _ptr(v), n, _ptr(path), _ptr(n_path), m, _ptr(counts), self.s)
+
+    # ---- beams (mkv_cache_reorder) -------------------------------------------------------------
+    def reorder(self, parent, width):
+        """Beam w of group g takes the state of beam parent[g * width + w] (int32 [S]) of its group."""
+        check_tensor("parent", parent, self.arena.device, self.torch.int32, (self.S,))
+        L.mkv_cache_reorder(self.h, _ptr(parent), width, self.s)
 
     # ---- inspection --------------------------------------------------------------------------
     def export(self, seq, kv_head, what, dtype=None):

@@ -1,0 +1,352 @@
+// Beam selection: the best continuations of every request's beams.
+//
+// A continuation (w, t) scores scores[w] + logit(w, t) - lse(w).  Within a beam that order is the
+// logits' own, so one pass over the logits is enough: each workgroup takes a chunk of one beam's
+// vocabulary into registers and writes the chunk's best n_select logits, its maximum and its sum of
+// exponentials; a second, small launch has every request's candidates compared by their full scores
+// in float64 (two beams' scores lie closer than float32 tells apart once in some thousand selections).
+// Bound by reading the logits once.
+//
+// Choosing the best K of a workgroup's values: every value has a unique 64-bit key (order-preserving
+// bits of the value, then the lower index first).  The keys' maxima over groups of 16 lanes are 64 keys
+// of the workgroup, and the K-th largest of these (K <= 64) is not above the K-th largest key of
+// all: only the values that reach it (about K of random ones, at most the values of K groups) are
+// collected and ranked against each other.  Where they do not fit the list (values in ascending order, or
+// constant), the best ones are taken one after another.
+#include <algorithm>
+
+#include "kernels_common.h"
+#include "mkv_decoding.h"
+
+namespace mkv {
+
+namespace {
+
+constexpr int kBeamWaves = kBeamThreads / 64;
+constexpr int kBeamGroups = kBeamThreads / 16;
+constexpr int kListCap = 2048;
+static_assert(2 * MKV_BEAM_MAX <= kBeamGroups && kBeamGroups == 64, "the K-th largest group maximum is taken by one wave");
+
+typedef unsigned long long u64;
+
+// Largest key over each row of 16 lanes, in all its lanes.
+MKV_DEV u64 row_max_u64(u64 x) {
+  auto step = [&](auto ctrl) {
+    constexpr int C = decltype(ctrl)::value;
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, C, 0xF, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), C, 0xF, 0xF, false);
+    const u64 y = ((u64)hi << 32) | lo;
+    x = y > x ? y : x;
+  };
+  step(std::integral_constant<int, 0xB1>{});
+  step(std::integral_constant<int, 0x4E>{});
+  step(std::integral_constant<int, 0x141>{});
+  step(std::integral_constant<int, 0x140>{});
+  return x;
+}
+
+// The K-th largest of the 64 values in `s` (by lane order among equals), for one whole wave.
+MKV_DEV u64 kth_of_64(const u64 *s, int k) {
+  const int lane = threadIdx.x & 63;
+  const u64 mine = s[lane];
+  int above = 0;
+  for (int i = 0; i < 64; ++i) {
+    const u64 o = s[i];
+    above += (o > mine || (o == mine && i < lane)) ? 1 : 0;
+  }
+  const u64 hit = __ballot(above == k - 1);  // exactly one lane
+  return s[__builtin_ctzll(hit)];
+}
+
+struct PickLds {
+  u64 group[kBeamGroups];
+  u64 tau;
+  int n;
+};
+
+// The keys of a chunk's values: high word the value's order, low word the lower index first; 0: no value.
+MKV_DEV u64 chunk_key(float x, int index) { return ((u64)float_key(x) << 32) | (uint32_t)~index; }
+
+// One workgroup per (chunk, row): E values a thread, in pieces of 4 contiguous ones.
+template <typename T, int E>
+__global__ __launch_bounds__(kBeamThreads) void k_beam_scan(const T *__restrict__ logits, int64_t row_stride, int vocab,
+                                                            int k, int n_chunks, BeamPartial *__restrict__ parts,
+                                                            BeamCandidate *__restrict__ cands) {
+  __shared__ PickLds L;
+  __shared__ u64 s_list[kListCap];
+  __shared__ float s_max[kBeamWaves];
+  __shared__ double s_sum[kBeamWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int chunk = blockIdx.x % n_chunks;
+  const int64_t row = blockIdx.x / n_chunks;
+  const T *p = logits + row * row_stride;
+  const int base = chunk * kBeamThreads * E;
+  float x[E];
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i) {
+    const int at = base + (i * kBeamThreads + tid) * 4;
+    float *f = x + 4 * i;
+    if (at + 4 <= vocab) {
+      if constexpr (sizeof(T) == 4) {
+        const uint4 u = gld16w(reinterpret_cast<const uint32_t *>(p) + at);
+        f[0] = __builtin_bit_cast(float, u.x);
+        f[1] = __builtin_bit_cast(float, u.y);
+        f[2] = __builtin_bit_cast(float, u.z);
+        f[3] = __builtin_bit_cast(float, u.w);
+      } else {
+        typedef uint32_t u32x2h __attribute__((ext_vector_type(2), aligned(2)));
+        const u32x2h u = *(const MKV_GLOBAL u32x2h *)(p + at);
+        f[0] = h2f(u[0]);
+        f[1] = h2f(u[0] >> 16);
+        f[2] = h2f(u[1]);
+        f[3] = h2f(u[1] >> 16);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        f[j] = -INFINITY;
+        if (at + j < vocab) {
+          if constexpr (sizeof(T) == 4) f[j] = gld(p + at + j);
+          else f[j] = h2f(gld(p + at + j));
+        }
+      }
+    }
+  }
+  float mx = -INFINITY;
+  u64 best = 0;
+  auto key_of = [&](int i, float v) { return chunk_key(v, base + ((i >> 2) * kBeamThreads + tid) * 4 + (i & 3)); };
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    if (!(x[i] > -INFINITY)) x[i] = -INFINITY;  // NaN
+    mx = fmaxf(mx, x[i]);
+  }
+#pragma unroll
+  for (int i = E - 1; i >= 0; --i) best = x[i] == mx ? key_of(i, x[i]) : best;  // the lowest index of the maximum
+  if (mx == -INFINITY) best = 0;
+  const u64 gm = row_max_u64(best);
+  if ((lane & 15) == 0) L.group[tid >> 4] = gm;
+  const float wm = wave_max(mx);
+  if (lane == 0) s_max[wave] = wm;
+  if (tid == 0) L.n = 0;
+  __syncthreads();
+  float M = s_max[0];
+#pragma unroll
+  for (int w = 1; w < kBeamWaves; ++w) M = fmaxf(M, s_max[w]);
+  if (wave == 0) {
+    const u64 t = kth_of_64(L.group, k);
+    if (lane == 0) L.tau = t;
+  }
+  // the sum of exponentials: float32 over a thread's values, float64 over the threads
+  float sum = 0.f;
+  if (M != -INFINITY) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) sum += fexp2((x[i] - M) * kLog2e);
+  }
+  double ds = sum;
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) ds += __shfl_xor(ds, m);
+  if (lane == 0) s_sum[wave] = ds;
+  __syncthreads();
+  const u64 tau = L.tau;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    if (x[i] == -INFINITY) continue;
+    const u64 key = key_of(i, x[i]);
+    if (key >= tau) {
+      const int at = atomicAdd(&L.n, 1);
+      if (at < kListCap) s_list[at] = key;
+    }
+  }
+  __syncthreads();
+  const int n = L.n;
+  BeamCandidate *out = cands + (row * n_chunks + chunk) * k;
+  if (n <= kListCap) {
+    for (int i = tid; i < n; i += kBeamThreads) {
+      const u64 mine = s_list[i];
+      int above = 0;
+      for (int j = 0; j < n; ++j) above += s_list[j] > mine ? 1 : 0;
+      if (above < k) {
+        const int token = (int)~(uint32_t)mine;
+        const uint32_t o = (uint32_t)(mine >> 32);
+        out[above] = {__builtin_bit_cast(float, (o & 0x80000000u) ? o ^ 0x80000000u : ~o), token};
+      }
+    }
+    if (tid < k && tid >= n) out[tid] = {-INFINITY, -1};
+  } else {
+    // one after another: the largest key below the last one
+    u64 last = ~0ull;
+    for (int r = 0; r < k; ++r) {
+      u64 top = 0;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const u64 key = x[i] == -INFINITY ? 0 : key_of(i, x[i]);
+        top = key < last && key > top ? key : top;
+      }
+      const u64 g = row_max_u64(top);
+      __syncthreads();
+      if ((lane & 15) == 0) L.group[tid >> 4] = g;
+      __syncthreads();
+      u64 all = 0;
+      for (int i = 0; i < kBeamGroups; ++i) all = L.group[i] > all ? L.group[i] : all;
+      last = all;  // (n > kListCap >= k values are there)
+      if (tid == 0) {
+        const uint32_t o = (uint32_t)(all >> 32);
+        out[r] = {__builtin_bit_cast(float, (o & 0x80000000u) ? o ^ 0x80000000u : ~o), (int)~(uint32_t)all};
+      }
+    }
+  }
+  if (tid == 0) {
+    double total = 0.0;
+    for (int w = 0; w < kBeamWaves; ++w) total += s_sum[w];
+    parts[row * n_chunks + chunk] = {total, M, 0};
+  }
+}
+
+// A candidate's place in the order of a request: score (order-preserving bits), then the lower index.
+struct Rank {
+  u64 score, index;  // score 0: not above -infinity
+};
+MKV_DEV bool above(const Rank &a, const Rank &b) { return a.score > b.score || (a.score == b.score && a.index < b.index); }
+MKV_DEV u64 double_key(double x) {
+  if (!(x > -INFINITY)) return 0;
+  x += 0.0;  // -0 is +0
+  const u64 u = __builtin_bit_cast(u64, x);
+  return u >> 63 ? ~u : u | 0x8000000000000000ull;
+}
+MKV_DEV double key_double(u64 k) { return __builtin_bit_cast(double, k >> 63 ? k ^ 0x8000000000000000ull : ~k); }
+
+MKV_DEV Rank row_best(Rank x) {
+#pragma unroll
+  for (int m = 1; m < 16; m <<= 1) {
+    const Rank y = {(u64)__shfl_xor((long long)x.score, m), (u64)__shfl_xor((long long)x.index, m)};
+    if (above(y, x)) x = y;
+  }
+  return x;
+}
+
+// One workgroup per request.
+__global__ __launch_bounds__(kBeamThreads) void k_beam_merge(BeamArgs a, const BeamPartial *__restrict__ parts,
+                                                             const BeamCandidate *__restrict__ cands, int n_chunks) {
+  __shared__ double s_base[MKV_BEAM_MAX];  // scores[w] - lse(w); a finished beam: scores[w]
+  __shared__ int s_done[MKV_BEAM_MAX];
+  __shared__ Rank s_group[kBeamGroups];
+  __shared__ Rank s_list[kListCap / 2];
+  __shared__ Rank s_tau;
+  __shared__ int s_n;
+  constexpr int kCap = kListCap / 2;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int b = blockIdx.x, W = a.n_beams, K = a.n_select;
+  if (tid == 0) s_n = 0;
+  for (int w = wave; w < W; w += kBeamWaves) {
+    const int64_t row = (int64_t)b * W + w;
+    float m = -INFINITY;
+    for (int c = lane; c < n_chunks; c += 64) m = fmaxf(m, parts[row * n_chunks + c].max);
+    m = wave_max(m);
+    double sum = 0.0;
+    for (int c = lane; c < n_chunks; c += 64) {
+      const BeamPartial p = parts[row * n_chunks + c];
+      if (p.max != -INFINITY) sum += p.sum * exp((double)p.max - (double)m);
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) {
+      const int done = a.finished && a.finished[row] ? 1 : 0;
+      s_done[w] = done;
+      s_base[w] = (double)a.scores[row] - (done ? 0.0 : (double)m + log(sum));
+    }
+  }
+  __syncthreads();
+  // candidate i: beam i / per, the i % per-th of its chunks' candidates
+  const int per = n_chunks * K, total = W * per;
+  auto rank_of = [&](int i) {
+    const int w = i / per, j = i % per;
+    if (s_done[w])
+      return j == 0 ? Rank{double_key(s_base[w]), (u64)w * a.vocab + a.pad_token} : Rank{0, ~0ull};
+    const BeamCandidate c = cands[((int64_t)b * W + w) * per + j];
+    if (c.token < 0) return Rank{0, ~0ull};
+    return Rank{double_key(s_base[w] + (double)c.logit), (u64)w * a.vocab + c.token};
+  };
+  Rank best = {0, ~0ull};
+  for (int i = tid; i < total; i += kBeamThreads) {
+    const Rank r = rank_of(i);
+    if (above(r, best)) best = r;
+  }
+  best = row_best(best);
+  if ((lane & 15) == 0) s_group[tid >> 4] = best;
+  __syncthreads();
+  if (wave == 0) {  // the K-th best group
+    const Rank mine = s_group[lane];
+    int n = 0;
+    for (int i = 0; i < kBeamGroups; ++i) {
+      const Rank o = s_group[i];
+      n += above(o, mine) || (o.score == mine.score && o.index == mine.index && i < lane) ? 1 : 0;
+    }
+    if (n == K - 1) s_tau = mine;
+  }
+  __syncthreads();
+  const Rank tau = s_tau;
+  for (int i = tid; i < total; i += kBeamThreads) {
+    const Rank r = rank_of(i);
+    if (r.score != 0 && !above(tau, r)) {
+      const int at = atomicAdd(&s_n, 1);
+      if (at < kCap) s_list[at] = r;
+    }
+  }
+  __syncthreads();
+  const int n = s_n;
+  auto write = [&](int at, const Rank &r) {
+    const int64_t o = (int64_t)b * K + at;
+    a.token[o] = r.score ? (int)(r.index % a.vocab) : a.pad_token;
+    a.parent[o] = r.score ? (int)(r.index / a.vocab) : 0;
+    a.score_out[o] = r.score ? (float)key_double(r.score) : -INFINITY;
+  };
+  if (n <= kCap) {
+    for (int i = tid; i < n; i += kBeamThreads) {
+      const Rank mine = s_list[i];
+      int before = 0;
+      for (int j = 0; j < n; ++j) before += above(s_list[j], mine) ? 1 : 0;
+      if (before < K) write(before, mine);
+    }
+    if (tid < K && tid >= n) write(tid, Rank{0, 0});
+  } else {
+    Rank last = {~0ull, 0};
+    for (int r = 0; r < K; ++r) {
+      Rank top = {0, ~0ull};
+      for (int i = tid; i < total; i += kBeamThreads) {
+        const Rank c = rank_of(i);
+        if (above(last, c) && above(c, top)) top = c;
+      }
+      top = row_best(top);
+      __syncthreads();
+      if ((lane & 15) == 0) s_group[tid >> 4] = top;
+      __syncthreads();
+      Rank all = s_group[0];
+      for (int i = 1; i < kBeamGroups; ++i)
+        if (above(s_group[i], all)) all = s_group[i];
+      last = all;
+      if (tid == 0) write(r, all);
+    }
+  }
+}
+
+template <typename T>
+hipError_t beam_impl(const BeamArgs &a, hipStream_t st) {
+  const int rows = a.n_batch * a.n_beams, chunks = beam_chunks(rows, a.vocab);
+  BeamPartial *parts = static_cast<BeamPartial *>(a.workspace);
+  BeamCandidate *cands = reinterpret_cast<BeamCandidate *>(parts + (int64_t)rows * chunks);
+  auto kernel = beam_values(rows, a.vocab) == 16 ? k_beam_scan<T, 16> : k_beam_scan<T, 4>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)rows * chunks)), dim3(kBeamThreads), 0, st,
+                     static_cast<const T *>(a.logits), a.row_stride, a.vocab, a.n_select, chunks, parts, cands);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_beam_merge, dim3(a.n_batch), dim3(kBeamThreads), 0, st, a, parts, cands, chunks);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_beam_select(const BeamArgs &a, hipStream_t st) {
+  return a.half ? beam_impl<uint16_t>(a, st) : beam_impl<float>(a, st);
+}
+
+}  // namespace mkv

@@ -1,0 +1,785 @@
+// Drafted trees: attention of several drafted tokens per sequence over its cache and over each other, and
+// the append of those that are accepted.
+//
+// Attention.  The query rows of a (sequence, kv head) are its nodes' query heads, N G of them; all
+// attend to the same cached tokens, so their logits and outputs are matrix products.  A workgroup takes
+// R rows and a range of 64-token tiles; the last range ends with one more tile, the tree's own keys and
+// values under the nodes' masks.  A tile is brought into LDS as fp16 rows, whatever the method it is
+// stored under (each code is dequantized once per workgroup and serves all its rows; outliers replace
+// their values there), keys as [token][channel], values as [channel][token], which are the two products'
+// operands:
+//   S^T = K Q^T (tokens x rows),  O^T = V^T P^T (channels x rows)
+// with v_mfma_f32_16x16x32_f16.  S^T's result layout (tokens 4 (lane / 16) + i, row lane % 16) is P^T's
+// operand layout up to the order of the tokens, which the value reads follow, so probabilities stay in
+// their lanes.  One pass: running maximum and sum per row in float32; ranges are merged by their
+// maxima, waves through LDS and splits by a second launch.
+//
+// Roundings to fp16: dequantized keys and values (half a step, 2^-12 of the value on average; fp16 rows
+// and outliers exact), uniform steps before they multiply a code (2^-11 of it), and probabilities,
+// which are at most 2^kLazy at the running reference.  Everything summed is float32.
+#include <algorithm>
+
+#include "append_dev.h"
+#include "mkv_decoding.h"
+
+namespace mkv {
+
+namespace {
+
+constexpr int kTreeThreads = 256;
+constexpr int kTile = kTreeTile;
+constexpr float kLazy = 2.f;  // the reference of a row's softmax moves when a logit passes it by this (log2)
+
+typedef _Float16 h2v __attribute__((ext_vector_type(2)));
+typedef _Float16 h4v __attribute__((ext_vector_type(4)));
+typedef _Float16 h8v __attribute__((ext_vector_type(8)));
+typedef float f4v __attribute__((ext_vector_type(4)));
+
+MKV_DEV f4v mfma32(h8v a, h8v b, f4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+MKV_DEV f4v mfma16(h4v a, h4v b, f4v c) { return __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0); }
+MKV_DEV uint32_t pk_lo(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+MKV_DEV uint32_t pk_hi(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+MKV_DEV uint32_t pk_f16(float lo, float hi) { return __builtin_bit_cast(uint32_t, h2v{(_Float16)lo, (_Float16)hi}); }
+MKV_DEV uint32_t pk_mul(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2v, a) * __builtin_bit_cast(h2v, b));
+}
+MKV_DEV uint32_t pk_fma(uint32_t a, uint32_t b, uint32_t c) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(h2v, a), __builtin_bit_cast(h2v, b),
+                                                                __builtin_bit_cast(h2v, c)));
+}
+// the 4-bit nibbles k and k + 4 of w (k < 4), each less 8, as a packed pair of exact fp16 integers: set
+// into the mantissa of 1024 (or, 4 bits up, of 64), which is then taken off with the 8
+MKV_DEV uint32_t nib_pair(uint32_t w, int k) {
+  const uint32_t x = k >= 2 ? w >> 8 : w;
+  const bool up = k & 1;
+  const uint32_t y = (x & (up ? 0x00F000F0u : 0x000F000Fu)) | (up ? 0x54005400u : 0x64006400u);
+  const _Float16 base = up ? (_Float16)72.0f : (_Float16)1032.0f;
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2v, y) - h2v{base, base});
+}
+
+// A tile in LDS.  Value rows hold 16 blocks of 4 tokens, block b of channel c at b ^ vswz(c): the writers
+// (16 channel groups at one block) and the readers (16 channels at one block) both spread over all banks.
+template <int D>
+struct Tile {
+  static constexpr int KS = D + 8;  // key row stride (halves)
+  uint16_t k[kTile * KS];
+  uint16_t v[D * kTile];
+};
+MKV_DEV int vswz(int ch) { return (ch ^ (ch >> 3)) & 15; }
+template <int D>
+MKV_DEV uint16_t *v_at(Tile<D> &t, int ch, int block) { return t.v + ch * kTile + 4 * (block ^ vswz(ch)); }
+template <int D>
+MKV_DEV void put_v(Tile<D> &t, int ch, int block, uint32_t t01, uint32_t t23) {
+  *reinterpret_cast<uint2 *>(v_at(t, ch, block)) = make_uint2(t01, t23);
+}
+template <int D>
+MKV_DEV void put_k8(Tile<D> &t, int token, int ch, const uint32_t *w) {
+  *reinterpret_cast<uint4 *>(t.k + token * Tile<D>::KS + ch) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// ---- tile loaders: fetch(tile, raw) reads a tile's data into registers, put(tile, raw, lds) writes it as
+// fp16 rows, fix(tile, raw, lds) (after a barrier; kFix) writes what replaces some of them.  Tokens at or
+// past `n` get value rows of zero (their probabilities are 0, and 0 x anything must stay 0).
+
+// fp16 rows `stride` elements apart: a cache's, or the drafted ones
+template <int D>
+struct RowsLoader {
+  static constexpr bool kFix = false;
+  static constexpr int NK = D / 32, VPL = D / 16;  // key pieces, value channels per thread
+  const uint16_t *K, *V;
+  int64_t stride;
+  int n;
+  struct Raw {
+    uint4 k[NK];
+    uint32_t v[4][VPL / 2];
+  };
+  MKV_DEV void fetch(int tile, Raw &r) const {
+    const int tid = threadIdx.x, last = n - 1;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const int t = min(tile * kTile + tid / (D / 8) + i * (2048 / D), last);
+      r.k[i] = gld16h(K + t * stride + 8 * (tid % (D / 8)));
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int t = min(tile * kTile + 4 * (tid >> 4) + j, last);
+      const uint16_t *p = V + t * stride + VPL * (tid & 15);
+      if constexpr (VPL == 8) {
+        const uint4 u = gld16h(p);
+        r.v[j][0] = u.x;
+        r.v[j][1] = u.y;
+        r.v[j][2] = u.z;
+        r.v[j][3] = u.w;
+      } else {
+        typedef uint32_t u32x2h __attribute__((ext_vector_type(2), aligned(2)));
+        const u32x2h u = *(const MKV_GLOBAL u32x2h *)p;
+        r.v[j][0] = u[0];
+        r.v[j][1] = u[1];
+      }
+    }
+  }
+  MKV_DEV void put(int tile, const Raw &r, Tile<D> &t) const {
+    const int tid = threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const uint32_t w[4] = {r.k[i].x, r.k[i].y, r.k[i].z, r.k[i].w};
+      put_k8(t, tid / (D / 8) + i * (2048 / D), 8 * (tid % (D / 8)), w);
+    }
+    const int b = tid >> 4, left = n - (tile * kTile + 4 * b);
+#pragma unroll
+    for (int i = 0; i < VPL / 2; ++i) {
+      uint32_t x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = j < left ? r.v[j][i] : 0u;
+      const int ch = VPL * (tid & 15) + 2 * i;
+      put_v(t, ch, b, pk_lo(x[0], x[1]), pk_lo(x[2], x[3]));
+      put_v(t, ch + 1, b, pk_hi(x[0], x[1]), pk_hi(x[2], x[3]));
+    }
+  }
+};
+
+// Uniform 4-bit: a tile is one 64-token key block, the last one of an incomplete block fp16 rows.  A
+// value is (min + 8 step) + (code - 8) step, one fused operation a pair in fp16: taken from the middle of
+// the group's range, the step's rounding weighs as much as the value's own (from its minimum, codes of 7
+// or 8 times the step would carry 2.5 times that into values near 0).
+template <int D>
+struct UqLoader {
+  static constexpr bool kFix = false;
+  static constexpr int NK = D / 32, NGRP = D / 64, NW = D / 32;
+  const uint8_t *kc, *vc;
+  const float *kmeta, *vmeta;
+  const uint16_t *kres;
+  int n;
+  struct Raw {
+    uint4 k[NK];     // codes of 8 channels in .x, or 8 fp16 keys
+    uint4 km[4];     // (min, step) of the thread's 8 channels
+    uint32_t v[NW];  // codes of D / 16 channels x 4 tokens
+    float2 vm[4][NGRP];
+  };
+  MKV_DEV void fetch(int tile, Raw &r) const {
+    const int tid = threadIdx.x, w = tid % (D / 8);
+    const bool whole = (tile + 1) * kTile <= n;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const int t = tid / (D / 8) + i * (2048 / D);
+      if (whole) r.k[i].x = gld(reinterpret_cast<const uint32_t *>(kc + (int64_t)(tile * kTile + t) * (D / 2)) + w);
+      else r.k[i] = gld16(kres + t * D + 8 * w);
+    }
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.km[i] = gld16(kmeta + ((int64_t)tile * D + 8 * w + 2 * i) * 2);
+    }
+    const int t0 = min(tile * kTile + 4 * (tid >> 4), (n - 1) & ~3);  // (slots come in fours)
+    const uint32_t *vp = reinterpret_cast<const uint32_t *>(vc + (int64_t)t0 * (D / 2) + (tid & 15) * (D / 8));
+#pragma unroll
+    for (int i = 0; i < NW; ++i) r.v[i] = gld(vp + i);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int g = 0; g < NGRP; ++g) {
+        const float *p = vmeta + ((int64_t)(t0 + j) * NGRP + g) * 2;
+        r.vm[j][g] = make_float2(gld(p), gld(p + 1));
+      }
+  }
+  MKV_DEV void put(int tile, const Raw &r, Tile<D> &t) const {
+    const int tid = threadIdx.x, w = tid % (D / 8);
+    if ((tile + 1) * kTile <= n) {
+      uint32_t mid[4], st[4];  // channels (0, 4), (1, 5), (2, 6), (3, 7) of the thread's 8
+      float m[8], s[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        m[2 * i] = __builtin_bit_cast(float, r.km[i].x);
+        s[2 * i] = __builtin_bit_cast(float, r.km[i].y);
+        m[2 * i + 1] = __builtin_bit_cast(float, r.km[i].z);
+        s[2 * i + 1] = __builtin_bit_cast(float, r.km[i].w);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        mid[i] = pk_f16(m[i] + 8.f * s[i], m[i + 4] + 8.f * s[i + 4]);
+        st[i] = pk_f16(s[i], s[i + 4]);
+      }
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        uint32_t x[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[c] = pk_fma(nib_pair(r.k[i].x, c), st[c], mid[c]);
+        const uint32_t o[4] = {pk_lo(x[0], x[1]), pk_lo(x[2], x[3]), pk_hi(x[0], x[1]), pk_hi(x[2], x[3])};
+        put_k8(t, tid / (D / 8) + i * (2048 / D), 8 * w, o);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        const uint32_t o[4] = {r.k[i].x, r.k[i].y, r.k[i].z, r.k[i].w};
+        put_k8(t, tid / (D / 8) + i * (2048 / D), 8 * w, o);
+      }
+    }
+    const int b = tid >> 4, rr = tid & 15, left = n - (tile * kTile + 4 * b);
+#pragma unroll
+    for (int g = 0; g < NGRP; ++g) {
+      float mid[4], st[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        mid[j] = j < left ? r.vm[j][g].x + 8.f * r.vm[j][g].y : 0.f;
+        st[j] = j < left ? r.vm[j][g].y : 0.f;
+      }
+      const uint32_t m01 = pk_f16(mid[0], mid[1]), m23 = pk_f16(mid[2], mid[3]);
+      const uint32_t s01 = pk_f16(st[0], st[1]), s23 = pk_f16(st[2], st[3]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {  // channel 64 g + 4 rr + c: operand 4 g + c of the segment
+        const uint32_t word = r.v[(4 * g + c) >> 1];
+        put_v(t, 64 * g + 4 * rr + c, b, pk_fma(nib_pair(word, 2 * (c & 1)), s01, m01),
+              pk_fma(nib_pair(word, 2 * (c & 1) + 1), s23, m23));
+      }
+    }
+  }
+};
+
+// KVQuant: codes through tables of fp16 pairs (or, at 2 bits, quads), times the channel's threshold
+// (keys) or the token's scale (values), which are fp16 values themselves; then the outliers.
+template <int D, int BITS>
+struct KvqLoader {
+  static constexpr bool kFix = true;
+  static constexpr int UK = kTile * D / 32, UV = kTile / 4 * D / 8;  // units of 32 keys, of 8 channels x 4 tokens
+  const uint8_t *kc, *vc;
+  const uint32_t *krow, *kout, *vout;
+  const float *vsc;
+  const uint32_t *lutk, *lutv;  // LDS
+  const uint32_t *tau;          // LDS: thresholds of channel pairs
+  int n, cap, nov, rowbytes;
+  bool outliers;
+  struct Raw {
+    uint32_t k[BITS], v[BITS];
+    float s[4];
+    uint32_t e0, e1, emid;  // the tile's range of key outliers, and where its second 32 tokens begin
+  };
+  MKV_DEV void fetch(int tile, Raw &r) const {
+    const int tid = threadIdx.x;
+    if (UK == kTreeThreads || tid < UK) {
+      const int t = min(tile * kTile + tid / (D / 32), n - 1);
+      const uint32_t *p = reinterpret_cast<const uint32_t *>(kc + (int64_t)t * rowbytes) + BITS * (tid % (D / 32));
+#pragma unroll
+      for (int i = 0; i < BITS; ++i) r.k[i] = gld(p + i);
+    }
+    if (UV == kTreeThreads || tid < UV) {
+      const int t0 = min(tile * kTile + 4 * (tid / (D / 8)), (n - 1) & ~3);
+      const uint32_t *p = reinterpret_cast<const uint32_t *>(vc + (int64_t)t0 * rowbytes) + BITS * (tid % (D / 8));
+#pragma unroll
+      for (int i = 0; i < BITS; ++i) r.v[i] = gld(p + i);
+      const U4 s = gld16u(vsc + t0);
+      r.s[0] = __builtin_bit_cast(float, s.x);
+      r.s[1] = __builtin_bit_cast(float, s.y);
+      r.s[2] = __builtin_bit_cast(float, s.z);
+      r.s[3] = __builtin_bit_cast(float, s.w);
+    }
+    r.e0 = gld(krow + tile * kTile);
+    r.emid = gld(krow + min(tile * kTile + 32, n));
+    r.e1 = gld(krow + min(tile * kTile + 64, n));
+  }
+  // bits [at, at + 2 BITS) of a unit, as the packed pair they stand for
+  MKV_DEV uint32_t pair(const uint32_t *lut, const uint32_t (&w)[BITS], int f) const {
+    const int bit = 2 * BITS * f, i = bit >> 5, s = bit & 31;
+    const uint32_t x = s + 2 * BITS <= 32 ? w[i] >> s : __builtin_amdgcn_alignbit(w[min(i + 1, BITS - 1)], w[i], s);
+    return lut[x & ((1 << (2 * BITS)) - 1)];
+  }
+  // the quad of codes f as two packed pairs
+  MKV_DEV uint2 quad(const uint32_t *lut, const uint32_t (&w)[BITS], int f) const {
+    if constexpr (BITS == 2) return *reinterpret_cast<const uint2 *>(lut + 2 * ((w[f >> 2] >> (8 * (f & 3))) & 0xFFu));
+    else return make_uint2(pair(lut, w, 2 * f), pair(lut, w, 2 * f + 1));
+  }
+  MKV_DEV void put(int tile, const Raw &r, Tile<D> &t) const {
+    const int tid = threadIdx.x;
+    if (UK == kTreeThreads || tid < UK) {
+      const int token = tid / (D / 32), ch = 32 * (tid % (D / 32));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint2 a = quad(lutk, r.k, 2 * i), b = quad(lutk, r.k, 2 * i + 1);
+        const uint4 u = *reinterpret_cast<const uint4 *>(tau + ch / 2 + 4 * i);
+        const uint32_t o[4] = {pk_mul(a.x, u.x), pk_mul(a.y, u.y), pk_mul(b.x, u.z), pk_mul(b.y, u.w)};
+        put_k8(t, token, ch + 8 * i, o);
+      }
+    }
+    if (UV == kTreeThreads || tid < UV) {
+      const int b = tid / (D / 8), ch = 8 * (tid % (D / 8)), left = n - (tile * kTile + 4 * b);
+      float s[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j] = j < left ? r.s[j] : 0.f;
+      const uint32_t s01 = pk_f16(s[0], s[1]), s23 = pk_f16(s[2], s[3]);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const uint2 a = quad(lutv, r.v, c);
+        put_v(t, ch + c, b, pk_mul(a.x, s01), pk_mul(a.y, s23));
+      }
+    }
+  }
+  MKV_DEV void fix(int tile, const Raw &r, Tile<D> &t) const {
+    const int tid = threadIdx.x;
+    for (uint32_t e = r.e0 + tid; e < r.e1; e += kTreeThreads) {
+      const uint32_t x = gld(kout + e);
+      const int token = (outlier_tag(x) & 31) + (e >= r.emid ? 32 : 0);
+      t.k[token * Tile<D>::KS + min(outlier_ch(x), D - 1)] = (uint16_t)(x >> 16);
+    }
+    const int left = min(kTile, n - tile * kTile);
+    for (int i = tid; i < kTile * nov; i += kTreeThreads) {
+      const int token = i & 63;
+      if (token >= left) continue;
+      const uint32_t x = gld(vout + (int64_t)(i >> 6) * cap + tile * kTile + token);
+      if (x == kNoOutlier) continue;
+      v_at(t, min(outlier_ch(x), D - 1), token >> 2)[token & 3] = (uint16_t)(x >> 16);
+    }
+  }
+};
+
+// ---- the attention ------------------------------------------------------------------------------------
+// Waves: WR of them take 16 RB rows each, and WT = 4 / WR share a tile's tokens.
+template <int D, int RB, int WR>
+struct TG {
+  static constexpr int WT = 4 / WR, TW = kTile / WT, R = 16 * RB * WR;
+  static constexpr int NB = TW == 16 ? 1 : 2;  // 16-token blocks of one step
+  static constexpr int NM = D / 16, NQ = D / 32;
+};
+
+// A wave's rows: row 16 rb + lane % 16 of each lane, and what it has summed.
+template <int D, int RB, int WR>
+struct Rows {
+  using G_ = TG<D, RB, WR>;
+  h8v q[G_::NQ][RB];
+  f4v o[G_::NM][RB];
+  float m[RB], l[RB];
+  unsigned long long mask[RB];  // the nodes that the row attends to
+};
+
+// The wave's tokens of a tile in LDS: logits, softmax, output.  Tokens at or past `left` do not exist; TREE:
+// nor does, for a row, a token that its mask does not name.
+template <int D, int RB, int WR, bool TREE>
+MKV_DEV void attend_tile(Tile<D> &t, Rows<D, RB, WR> &x, int left, float qscale) {
+  using C = TG<D, RB, WR>;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lq = lane >> 4;
+  const int tok0 = (wave % C::WT) * C::TW;
+#pragma unroll
+  for (int u = 0; u < C::TW / (16 * C::NB); ++u) {
+    const int first = tok0 + 16 * C::NB * u;
+    f4v S[C::NB][RB];
+#pragma unroll
+    for (int b = 0; b < C::NB; ++b)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) S[b][rb] = f4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int m = 0; m < C::NQ; ++m)
+#pragma unroll
+      for (int b = 0; b < C::NB; ++b) {
+        const h8v a = *reinterpret_cast<const h8v *>(t.k + (first + 16 * b + lr) * Tile<D>::KS + 32 * m + 8 * lq);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) S[b][rb] = mfma32(a, x.q[m][rb], S[b][rb]);
+      }
+    float mx[RB];
+    bool move = false;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      mx[rb] = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < C::NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int token = first + 16 * b + 4 * lq + i;
+          const bool on = token < left && (!TREE || ((x.mask[rb] >> token) & 1));
+          S[b][rb][i] = on ? S[b][rb][i] * qscale : -INFINITY;
+          mx[rb] = fmaxf(mx[rb], S[b][rb][i]);
+        }
+      move |= mx[rb] > x.m[rb] + kLazy;
+    }
+    if (__any(move)) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        float y = fmaxf(mx[rb], __shfl_xor(mx[rb], 16));
+        y = fmaxf(y, __shfl_xor(y, 32));
+        const bool up = y > x.m[rb];
+        const float corr = up ? fexp2(x.m[rb] - y) : 1.f;
+        if (up) x.m[rb] = y;
+        x.l[rb] *= corr;
+#pragma unroll
+        for (int m = 0; m < C::NM; ++m) x.o[m][rb] *= corr;
+      }
+    }
+    uint32_t P[RB][2 * C::NB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int b = 0; b < C::NB; ++b) {
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // (a row that has seen nothing yet has no reference)
+          p[i] = S[b][rb][i] == -INFINITY ? 0.f : fexp2(S[b][rb][i] - x.m[rb]);
+          x.l[rb] += p[i];
+        }
+        P[rb][2 * b] = pk_f16(p[0], p[1]);
+        P[rb][2 * b + 1] = pk_f16(p[2], p[3]);
+      }
+#pragma unroll
+    for (int m = 0; m < C::NM; ++m) {
+      const int ch = 16 * m + lr;
+      const uint2 a0 = *reinterpret_cast<const uint2 *>(v_at(t, ch, first / 4 + lq));
+      if constexpr (C::NB == 2) {
+        const uint2 a1 = *reinterpret_cast<const uint2 *>(v_at(t, ch, first / 4 + 4 + lq));
+        const h8v a = __builtin_bit_cast(h8v, make_uint4(a0.x, a0.y, a1.x, a1.y));
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+          x.o[m][rb] = mfma32(a, __builtin_bit_cast(h8v, make_uint4(P[rb][0], P[rb][1], P[rb][2], P[rb][3])), x.o[m][rb]);
+      } else {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+          x.o[m][rb] = mfma16(__builtin_bit_cast(h4v, a0), __builtin_bit_cast(h4v, make_uint2(P[rb][0], P[rb][1])), x.o[m][rb]);
+      }
+    }
+  }
+}
+
+template <int D, int RB, int WR, class L>
+MKV_DEV void attend_range(const L &ld, Tile<D> &t, Rows<D, RB, WR> &x, int begin, int end, float qscale) {
+  typename L::Raw raw;
+  if (begin < end) ld.fetch(begin, raw);
+  for (int tile = begin; tile < end; ++tile) {
+    ld.put(tile, raw, t);
+    __syncthreads();
+    if constexpr (L::kFix) {
+      if (ld.outliers) {  // (the same in all threads)
+        ld.fix(tile, raw, t);
+        __syncthreads();
+      }
+    }
+    if (tile + 1 < end) ld.fetch(tile + 1, raw);
+    attend_tile<D, RB, WR, false>(t, x, ld.n - tile * kTile, qscale);
+    __syncthreads();
+  }
+}
+
+// What the kernel and the merge need to agree on.
+struct TreeGeo {
+  int Hkv, G, N, max_splits, chunk, max_new, items, row_blocks;
+};
+// Splits of sequence s (a tile range each, by its capacity), and its first slot among all sequences'.
+MKV_DEV int splits_of(const SeqDesc &sd, const TreeGeo &g) { return (sd.cap + g.chunk - 1) / g.chunk; }
+MKV_DEV int64_t first_split(const SeqDesc &sd, int s, const TreeGeo &g) {
+  // capacities are at most n0 + max_new + 3, so this many splits lie before it
+  return (sd.row0 + (int64_t)s * (g.max_new + 3)) / g.chunk + s;
+}
+// Tiles per split of a sequence that holds n tokens (its drafted tokens are the last tile).
+MKV_DEV int tiles_per_split(int n, int splits) { return ((n + kTile - 1) / kTile + 1 + splits - 1) / splits; }
+
+template <int D, int RB, int WR>
+__global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const SeqDesc *__restrict__ seqs,
+                                                            const int32_t *__restrict__ state,
+                                                            const float *__restrict__ cbtab, TreeArgs a, TreeGeo geo,
+                                                            float qscale) {
+  using C = TG<D, RB, WR>;
+  constexpr int R = C::R, WT = C::WT, NM = C::NM;
+  __shared__ __attribute__((aligned(16))) Tile<D> tile;
+  __shared__ __attribute__((aligned(16))) uint32_t s_lut[1024];
+  __shared__ __attribute__((aligned(16))) uint32_t s_tau[D / 2];
+  __shared__ float s_m[WT][R], s_l[WT][R];
+  static_assert(WT == 1 || sizeof(float) * R * D <= sizeof(tile), "the waves' outputs are merged in the tile");
+  const int item = blockIdx.x, yb = blockIdx.y;
+  if (item >= geo.items) return;
+  const int split = item % geo.max_splits, sh = item / geo.max_splits, h = sh % geo.Hkv, s = sh / geo.Hkv;
+  const SeqDesc &sd = seqs[s];
+  const int splits = splits_of(sd, geo);
+  if (split >= splits) return;
+  const int n = state[((int64_t)s * geo.Hkv + h) * ST_WORDS + ST_COUNT];
+  const int N = geo.N, G = geo.G, Hq = geo.Hkv * G;
+  const int valid = a.n_valid ? min(max(a.n_valid[s], 0), N) : N;
+  if (yb * R >= valid * G) return;
+  const int per = tiles_per_split(n, splits), tiles = (n + kTile - 1) / kTile;
+  const int begin = split * per, end = min(begin + per, tiles);
+  if (begin > tiles) return;
+  const bool tree = begin + per > tiles;  // the drafted tokens are tile number `tiles`
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lq = lane >> 4;
+  const int wr = wave / WT, wt = wave % WT;
+  Rows<D, RB, WR> x;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int row = yb * R + (wr * RB + rb) * 16 + lr, node = row / G;
+    const bool on = node < valid;
+    const uint16_t *qp = a.q + (((int64_t)s * N + (on ? node : 0)) * Hq + h * G + row % G) * D;
+#pragma unroll
+    for (int m = 0; m < C::NQ; ++m) {
+      const uint4 u = gld16h(qp + 32 * m + 8 * lq);
+      x.q[m][rb] = __builtin_bit_cast(h8v, on ? u : make_uint4(0u, 0u, 0u, 0u));
+    }
+    x.mask[rb] = on && tree ? gld(a.mask + (int64_t)s * N + node) : 0ull;
+    x.m[rb] = -INFINITY;
+    x.l[rb] = 0.f;
+#pragma unroll
+    for (int m = 0; m < NM; ++m) x.o[m][rb] = f4v{0.f, 0.f, 0.f, 0.f};
+  }
+  if (sd.method == FP16) {
+    RowsLoader<D> ld;
+    ld.K = reinterpret_cast<const uint16_t *>(sd.k) + h * stride_rows(sd, D);
+    ld.V = reinterpret_cast<const uint16_t *>(sd.v) + h * stride_rows(sd, D);
+    ld.stride = D;
+    ld.n = n;
+    attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale);
+  } else if (sd.method == UQ) {
+    UqLoader<D> ld;
+    ld.kc = reinterpret_cast<const uint8_t *>(sd.kc) + h * stride_codes(sd);
+    ld.vc = reinterpret_cast<const uint8_t *>(sd.vc) + h * stride_codes(sd);
+    ld.kmeta = reinterpret_cast<const float *>(sd.kmeta) + h * stride_uq_kmeta(sd, D) * 2;
+    ld.vmeta = reinterpret_cast<const float *>(sd.vmeta) + h * stride_uq_vmeta(sd, D) * 2;
+    ld.kres = reinterpret_cast<const uint16_t *>(sd.kres) + (int64_t)h * kTile * D;
+    ld.n = n;
+    attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale);
+  } else {
+    auto run = [&](auto bits_tag) {
+      constexpr int BITS = decltype(bits_tag)::value;
+      const uint32_t *lut = reinterpret_cast<const uint32_t *>(cbtab + kLutBase) + lut_offset(BITS);
+      for (int i = threadIdx.x; i < 2 * lut_half_words(BITS); i += kTreeThreads) s_lut[i] = gld(lut + i);
+      const float *tau = reinterpret_cast<const float *>(sd.kmeta) + (int64_t)h * D * 2;
+      if (threadIdx.x < D / 2) s_tau[threadIdx.x] = pk_f16(gld(tau + 4 * threadIdx.x), gld(tau + 4 * threadIdx.x + 2));
+      __syncthreads();
+      KvqLoader<D, BITS> ld;
+      ld.kc = reinterpret_cast<const uint8_t *>(sd.kc) + h * stride_codes(sd);
+      ld.vc = reinterpret_cast<const uint8_t *>(sd.vc) + h * stride_codes(sd);
+      ld.krow = reinterpret_cast<const uint32_t *>(sd.krow) + h * stride_krow(sd);
+      ld.kout = reinterpret_cast<const uint32_t *>(sd.kout) + h * stride_kout(sd);
+      ld.vout = reinterpret_cast<const uint32_t *>(sd.vout) + h * stride_vout(sd);
+      ld.vsc = reinterpret_cast<const float *>(sd.vmeta) + h * stride_slots(sd);
+      ld.lutk = s_lut;
+      ld.lutv = s_lut + lut_half_words(BITS);
+      ld.tau = s_tau;
+      ld.n = n;
+      ld.cap = sd.cap;
+      ld.nov = sd.nov_slots;
+      ld.rowbytes = sd.rowbytes;
+      ld.outliers = sd.bp > 0;
+      attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale);
+    };
+    if (sd.bits == 4) run(std::integral_constant<int, 4>{});
+    else if (sd.bits == 3) run(std::integral_constant<int, 3>{});
+    else run(std::integral_constant<int, 2>{});
+  }
+  if (tree) {
+    RowsLoader<D> ld;
+    ld.K = a.k + ((int64_t)s * N * geo.Hkv + h) * D;
+    ld.V = a.v + ((int64_t)s * N * geo.Hkv + h) * D;
+    ld.stride = (int64_t)geo.Hkv * D;
+    ld.n = valid;
+    typename RowsLoader<D>::Raw raw;
+    ld.fetch(0, raw);
+    // A value that is infinite or NaN must reach only the rows that attend to its node: it is left out
+    // of the product, where a probability of 0 would make it NaN, and added to those rows.
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const uint32_t w = raw.v[j][i];
+        const uint32_t bad = ((w & 0x7C00u) == 0x7C00u ? 0xFFFFu : 0u) | ((w & 0x7C000000u) == 0x7C000000u ? 0xFFFF0000u : 0u);
+        odd |= bad != 0u;
+        raw.v[j][i] = w & ~bad;
+      }
+    ld.put(0, raw, tile);
+    const bool any_odd = __syncthreads_or(odd);
+    attend_tile<D, RB, WR, true>(tile, x, valid, qscale);
+    if (any_odd && wt == 0) {
+      for (int j = 0; j < valid; ++j)
+#pragma unroll
+        for (int m = 0; m < NM; ++m)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w = gld(ld.V + j * ld.stride + 16 * m + 4 * lq + i);
+            if ((w & 0x7C00u) != 0x7C00u) continue;
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+              if ((x.mask[rb] >> j) & 1) x.o[m][rb][i] += h2f(w);
+          }
+    }
+    __syncthreads();
+  }
+  // a row's four quads hold disjoint tokens
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    x.l[rb] += __shfl_xor(x.l[rb], 16);
+    x.l[rb] += __shfl_xor(x.l[rb], 32);
+  }
+  if constexpr (WT > 1) {
+    // the waves that share rows: scaled to their common reference, then summed into the first
+    if (lq == 0) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        s_m[wt][(wr * RB + rb) * 16 + lr] = x.m[rb];
+        s_l[wt][(wr * RB + rb) * 16 + lr] = x.l[rb];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int row = (wr * RB + rb) * 16 + lr;
+      float M = s_m[0][row];
+#pragma unroll
+      for (int w = 1; w < WT; ++w) M = fmaxf(M, s_m[w][row]);
+      float Ls = 0.f;
+#pragma unroll
+      for (int w = 0; w < WT; ++w) Ls += s_m[w][row] == -INFINITY ? 0.f : s_l[w][row] * fexp2(s_m[w][row] - M);
+      const float f = x.m[rb] == -INFINITY ? 1.f : fexp2(x.m[rb] - M);  // (nothing summed: zeros)
+#pragma unroll
+      for (int m = 0; m < NM; ++m) x.o[m][rb] *= f;
+      x.m[rb] = M;
+      x.l[rb] = Ls;
+    }
+    float *red = reinterpret_cast<float *>(&tile);
+#pragma unroll 1
+    for (int w = 1; w < WT; ++w) {
+      if (wt == w) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+          for (int m = 0; m < NM; ++m)
+            *reinterpret_cast<f4v *>(red + ((((wr * RB + rb) * NM + m) * 64) + lane) * 4) = x.o[m][rb];
+      }
+      __syncthreads();
+      if (wt == 0) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+          for (int m = 0; m < NM; ++m)
+            x.o[m][rb] += *reinterpret_cast<const f4v *>(red + ((((wr * RB + rb) * NM + m) * 64) + lane) * 4);
+      }
+      __syncthreads();
+    }
+    if (wt != 0) return;
+  }
+  if (geo.max_splits == 1) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int row = yb * R + (wr * RB + rb) * 16 + lr, node = row / G;
+      if (node >= valid) continue;
+      const float inv = 1.f / x.l[rb];
+      uint16_t *op = a.out + (((int64_t)s * N + node) * Hq + h * G + row % G) * D;
+#pragma unroll
+      for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) gst(op + 16 * m + 4 * lq + i, f2h_bits(x.o[m][rb][i] * inv));
+    }
+    return;
+  }
+  float *part = a.workspace + (((first_split(sd, s, geo) + split) * geo.Hkv + h) * geo.row_blocks + yb) * (int64_t)(R * (D + 2));
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int row = (wr * RB + rb) * 16 + lr;
+#pragma unroll
+    for (int m = 0; m < NM; ++m) gst(reinterpret_cast<f4v *>(part + row * D + 16 * m + 4 * lq), x.o[m][rb]);
+    if (lq == 0) gst(reinterpret_cast<u32x2 *>(part + R * D + row * 2),
+                     u32x2{__builtin_bit_cast(uint32_t, x.m[rb]), __builtin_bit_cast(uint32_t, x.l[rb])});
+  }
+}
+
+// Merge of the splits: a thread takes 4 channels of a row.
+template <int D>
+__global__ __launch_bounds__(256) void k_tree_merge(const SeqDesc *__restrict__ seqs, const int32_t *__restrict__ state,
+                                                    TreeArgs a, TreeGeo geo, int R) {
+  constexpr int TPR = D / 4;  // threads per row
+  const int N = geo.N, G = geo.G, Hq = geo.Hkv * G;
+  const int blocks = (N * G + 256 / TPR - 1) / (256 / TPR);  // per (sequence, kv head)
+  const int sh = blockIdx.x / blocks, h = sh % geo.Hkv, s = sh / geo.Hkv;
+  const int row = (blockIdx.x % blocks) * (256 / TPR) + threadIdx.x / TPR, node = row / G, c = threadIdx.x % TPR * 4;
+  const int valid = a.n_valid ? min(max(a.n_valid[s], 0), N) : N;
+  if (node >= valid) return;
+  const SeqDesc &sd = seqs[s];
+  const int n = state[((int64_t)s * geo.Hkv + h) * ST_WORDS + ST_COUNT];
+  const int splits = splits_of(sd, geo), per = tiles_per_split(n, splits);
+  const int used = ((n + kTile - 1) / kTile + 1 + per - 1) / per;
+  const int64_t step = (int64_t)geo.Hkv * geo.row_blocks * R * (D + 2);
+  const float *part = a.workspace + ((first_split(sd, s, geo) * geo.Hkv + h) * geo.row_blocks + row / R) * (int64_t)(R * (D + 2));
+  const float *ml = part + R * D + (row % R) * 2, *o = part + (row % R) * D + c;
+  float M = -INFINITY;
+  for (int p = 0; p < used; ++p) M = fmaxf(M, gld(ml + p * step));
+  float Ls = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < used; ++p) {
+    const float m = gld(ml + p * step), l = gld(ml + p * step + 1);
+    const f4v v = gld(reinterpret_cast<const f4v *>(o + p * step));
+    const float w = m == -INFINITY ? 0.f : fexp2(m - M);
+    Ls += l * w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] += m == -INFINITY ? 0.f : v[i] * w;
+  }
+  uint16_t *op = a.out + (((int64_t)s * N + node) * Hq + h * G + row % G) * D + c;
+  const float inv = 1.f / Ls;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) gst(op + i, f2h_bits(acc[i] * inv));
+}
+
+template <int D, int RB, int WR>
+hipError_t tree_impl(const Dev &dv, const Shape &sh, const TreePlan &plan, const TreeArgs &a, hipStream_t st) {
+  const int items = sh.S * sh.Hkv * plan.max_splits;
+  const TreeGeo geo{sh.Hkv, sh.G, a.n_nodes, plan.max_splits, plan.chunk, sh.max_new, items, plan.row_blocks};
+  // the row blocks of a range are a multiple of 8 workgroups apart: on one XCD, whose L2 then holds the
+  // range for all of them
+  const dim3 grid((items + 7) & ~7, plan.row_blocks);
+  hipLaunchKernelGGL((k_tree_attn<D, RB, WR>), grid, dim3(kTreeThreads), 0, st, dv.seqs, dv.state, dv.cbtab, a, geo,
+                     kLog2e / sqrtf((float)D));
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || plan.max_splits == 1) return e;
+  constexpr int RPB = 256 / (D / 4);
+  const int blocks = (a.n_nodes * sh.G + RPB - 1) / RPB;
+  hipLaunchKernelGGL(k_tree_merge<D>, dim3(sh.S * sh.Hkv * blocks), dim3(256), 0, st, dv.seqs, dv.state, a, geo, plan.rows);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t tree_rows(const Dev &dv, const Shape &sh, const TreePlan &plan, const TreeArgs &a, hipStream_t st) {
+  switch (plan.rows) {
+    case 16: return tree_impl<D, 1, 1>(dv, sh, plan, a, st);
+    case 32: return tree_impl<D, 1, 2>(dv, sh, plan, a, st);
+    case 64: return tree_impl<D, 2, 2>(dv, sh, plan, a, st);
+    default: return tree_impl<D, 2, 4>(dv, sh, plan, a, st);
+  }
+}
+
+// ---- acceptance -----------------------------------------------------------------------------------------
+// One workgroup of D threads per (sequence, kv head) appends the path's tokens one after another (a token's
+// place among the outliers, its 4-token value block and its key block depend on the ones before).
+template <int D>
+__global__ __launch_bounds__(D) void k_tree_accept(const SeqDesc *__restrict__ seqs, int32_t *state,
+                                                   const uint16_t *__restrict__ k, const uint16_t *__restrict__ v,
+                                                   const float *__restrict__ cbtab, int Hkv, int n_nodes,
+                                                   const int32_t *__restrict__ path, const int32_t *__restrict__ n_path,
+                                                   int max_path, int32_t *counts) {
+  __shared__ AppendLds<D> L;
+  const int seq = blockIdx.x / Hkv, h = blockIdx.x % Hkv;
+  const SeqDesc &sd = seqs[seq];
+  int32_t *st = state + ((int64_t)seq * Hkv + h) * ST_WORDS;
+  int count = st[ST_COUNT], pos = st[ST_NEXT_POS];
+  const int take = min(max(n_path[seq], 0), max_path);
+  for (int i = 0; i < take; ++i) {
+    const int node = path[(int64_t)seq * max_path + i];
+    if (node < 0 || node >= n_nodes) break;
+    // load_token reads row `seq` of its k and v: the node's row is (seq (n_nodes - 1) + node) further
+    const int64_t ahead = ((int64_t)seq * (n_nodes - 1) + node) * Hkv * D;
+    const NewToken tok = load_token<D, D>(sd, st, seq, h, Hkv, k + ahead, v + ahead, cbtab, L);
+    if (!append_pair<D, D>(sd, st, tok, h, count, pos, count, -1, L)) break;
+    ++count;
+    ++pos;
+    // the next token reads what this one wrote (state, value block, key rows)
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    set_counts(st, count, pos);
+    if (counts != nullptr && h == 0) counts[seq] = count;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_tree_attention(const Dev &dv, const Shape &sh, const TreePlan &plan, const TreeArgs &a, hipStream_t st) {
+  return sh.D == 64 ? tree_rows<64>(dv, sh, plan, a, st) : tree_rows<128>(dv, sh, plan, a, st);
+}
+
+hipError_t launch_tree_accept(const Dev &dv, const Shape &sh, const uint16_t *k, const uint16_t *v, int n_nodes,
+                              const int32_t *path, const int32_t *n_path, int max_path, int32_t *counts, hipStream_t st) {
+  auto kernel = sh.D == 64 ? k_tree_accept<64> : k_tree_accept<128>;
+  hipLaunchKernelGGL(kernel, dim3(sh.S * sh.Hkv), dim3(sh.D), 0, st, dv.seqs, dv.state, k, v, dv.cbtab, sh.Hkv, n_nodes,
+                     path, n_path, max_path, counts);
+  return hipGetLastError();
+}
+
+}  // namespace mkv

@@ -12,7 +12,7 @@
 #include <vector>
 
 #include "mkv.h"
-#include "mkv_internal.h"
+#include "mkv_handle.h"
 
 using namespace mkv;
 
@@ -41,10 +41,6 @@ namespace {
 mkv_status hip_fail(hipError_t e, const char *what) {
   return fail(MKV_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
-
-enum Phase { PH_CREATED, PH_PROMPT, PH_READY, PH_APPENDED, PH_SELECTED, PH_ATTENDED };
-
-constexpr int kProfKinds = 5;
 
 struct Layout {
   std::vector<SeqDesc> seqs;  // offsets (relative to the arena) in the pointer fields
@@ -533,26 +529,6 @@ mkv_status make_layout(const mkv_shape *shp, const mkv_config *cfg, const int32_
 }
 
 }  // namespace
-
-struct mkv_cache {
-  Shape sh{};
-  std::vector<mkv_config> cfg;
-  std::vector<SeqDesc> hs;  // absolute device pointers
-  std::vector<SeqGroup> groups;
-  char *arena = nullptr;
-  Dev dv{};
-  Phase phase = PH_CREATED;
-  int steps = 0;
-  bool any_h2o = false, any_rocket = false, h2o_done = false, snap_done = false;
-  int topk_max = 0;
-  int h2o_rows = 0, rocket_rows = 0;
-  // profiling
-  bool evict_pending = false;  // H2O: the last eviction call's victims await the next decode append
-  int prof_mask = 0;  // bit k: launches of kind k are timed
-  int prof_cap = 0;
-  std::vector<hipEvent_t> ev[kProfKinds][2];
-  int prof_n[kProfKinds] = {};
-};
 
 namespace {
 

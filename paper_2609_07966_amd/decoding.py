@@ -1,0 +1,84 @@
+"""Torch-facing calls of the operators that need no cache: rotary positions and beam selection.
+
+PyTorch provides device memory and the stream; the work runs in libmkv's HIP kernels, on the
+current stream of the tensors' device.
+"""
+import torch
+
+from . import _lib as L
+from .cache import check_tensor
+
+
+def _rows(name, t, device):
+    if t.device != device or t.dtype != torch.float16 or t.dim() != 3:
+        raise ValueError(f"{name} must be float16 [rows][heads][head_dim] on {device}")
+    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError(f"{name}: a row's heads must be contiguous (rows may be any distance apart)")
+
+
+def rope(xs, pos, inv_freq, sections=None, layout="halves", inverse=False, out=None):
+    """Rotate the rows of each tensor of xs ([rows][heads][head_dim] fp16: a token's queries, its keys)
+    by their positions -> a list of outputs.
+
+    pos int32 [axes][rows]; inv_freq float32 [rotary_dim / 2]; sections: frequency pairs per axis
+    (default: all of the one axis); layout "halves" or "pairs"; inverse: turn back (the gradient).
+    out: tensors to write, which may be xs themselves (default: new ones)."""
+    dev = xs[0].device
+    n_rows, _, d = xs[0].shape
+    sections = [inv_freq.numel()] if sections is None else [int(n) for n in sections]
+    check_tensor("pos", pos, dev, torch.int32, (len(sections), n_rows))
+    check_tensor("inv_freq", inv_freq, dev, torch.float32, (sum(sections),))
+    if len(sections) > L.ROPE_MAX_AXES:
+        raise ValueError(f"at most {L.ROPE_MAX_AXES} axes (got {len(sections)})")
+    if layout not in L.ROPE_LAYOUTS:
+        raise ValueError(f"layout must be one of {sorted(L.ROPE_LAYOUTS)} (got {layout!r})")
+    if out is None:
+        out = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in xs]
+    if len(out) != len(xs):
+        raise ValueError("out has another number of tensors than xs")
+    sets = []
+    for x, y in zip(xs, out):
+        _rows("x", x, dev)
+        _rows("out", y, dev)
+        if x.shape != y.shape or x.shape[0] != n_rows or x.shape[2] != d:
+            raise ValueError("xs and out must agree in rows, heads and head_dim")
+        width = x.shape[1] * d
+        # (one row has any stride)
+        sets.append((x.data_ptr(), y.data_ptr(), x.stride(0) if n_rows > 1 else width,
+                     y.stride(0) if n_rows > 1 else width, x.shape[1]))
+    if n_rows > 0:
+        with torch.cuda.device(dev):
+            L.mkv_rope(d, 2 * sum(sections), sections, layout, inv_freq.data_ptr(), pos.data_ptr(), n_rows, sets, inverse,
+                       torch.cuda.current_stream(dev).cuda_stream)
+    return out
+
+
+def beam_workspace(n_batch, n_beams, vocab, n_select, device="cuda"):
+    """A workspace of beam_select, for calls that may overlap or be captured."""
+    return torch.empty(L.mkv_beam_workspace(n_batch, n_beams, vocab, n_select), dtype=torch.uint8, device=device)
+
+
+def beam_select(logits, scores, n_select, finished=None, pad_token=0, workspace=None):
+    """The n_select best continuations of each request's beams -> (token, parent int32, score float32),
+    each [batch][n_select], best first.
+
+    logits [batch][beams][vocab] float32 or float16 (rows may be any distance apart); scores float32
+    [batch][beams]; finished: optional uint8 [batch][beams], beams that continue with pad_token alone."""
+    dev = logits.device
+    b, w, v = logits.shape
+    if logits.dtype not in (torch.float32, torch.float16) or logits.stride(2) != 1 or \
+            (b > 1 and logits.stride(0) != w * logits.stride(1)):
+        raise ValueError("logits must be float32 or float16 with contiguous rows at one distance")
+    check_tensor("scores", scores, dev, torch.float32, (b, w))
+    if finished is not None:
+        check_tensor("finished", finished, dev, torch.uint8, (b, w))
+    stride = logits.stride(1) if w > 1 else logits.stride(0) if b > 1 else v
+    token = torch.empty((b, n_select), dtype=torch.int32, device=dev)
+    parent, score = torch.empty_like(token), torch.empty((b, n_select), dtype=torch.float32, device=dev)
+    ws = workspace if workspace is not None else beam_workspace(b, w, v, n_select, dev)
+    with torch.cuda.device(dev):
+        L.mkv_beam_select(logits.data_ptr(), L.F16 if logits.dtype == torch.float16 else L.F32, stride, b, w, v,
+                          scores.data_ptr(), 0 if finished is None else finished.data_ptr(), pad_token, n_select,
+                          token.data_ptr(), parent.data_ptr(), score.data_ptr(), ws.data_ptr(), ws.numel(),
+                          torch.cuda.current_stream(dev).cuda_stream)
+    return token, parent, score
