@@ -5,6 +5,7 @@ step runs in the library's HIP kernels; if the library is missing this module ra
 of ``lib()`` rather than falling back to anything else.
 """
 import ctypes
+import functools
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -261,12 +262,17 @@ def mkv_attention_tiles(h):
     return n.value, n_uq.value, n_rk.value
 
 
+@functools.lru_cache(maxsize=64)
+def _rope_spec(head_dim, rotary_dim, sections, layout):
+    return mkv_rope_spec(head_dim, rotary_dim, len(sections), (_I * ROPE_MAX_AXES)(*sections[:ROPE_MAX_AXES]),
+                         ROPE_LAYOUTS.get(layout, layout))
+
+
 def mkv_rope(head_dim, rotary_dim, sections, layout, inv_freq_ptr, pos_ptr, n_rows, sets, inverse, stream):
     """sets: sequence of (x pointer, y pointer, x row stride, y row stride, heads), strides in elements."""
-    spec = mkv_rope_spec(head_dim, rotary_dim, len(sections), (_I * ROPE_MAX_AXES)(*sections[:ROPE_MAX_AXES]),
-                         ROPE_LAYOUTS.get(layout, layout))
+    spec = _rope_spec(head_dim, rotary_dim, tuple(sections), layout)
     arr = (mkv_rope_set * len(sets))(*sets)
-    _check(lib().mkv_rope(ctypes.byref(spec), inv_freq_ptr, pos_ptr, n_rows, arr, len(sets), int(inverse), stream))
+    _check(lib().mkv_rope(spec, inv_freq_ptr, pos_ptr, n_rows, arr, len(sets), int(inverse), stream))
 
 
 def mkv_tree_workspace(h, n_nodes):
@@ -284,6 +290,7 @@ def mkv_tree_accept(h, k_ptr, v_ptr, n_nodes, path_ptr, n_path_ptr, max_path, co
     _check(lib().mkv_tree_accept(h, k_ptr, v_ptr, n_nodes, path_ptr, n_path_ptr, max_path, counts_ptr or None, stream))
 
 
+@functools.lru_cache(maxsize=64)
 def mkv_beam_workspace(n_batch, n_beams, vocab, n_select):
     n = ctypes.c_size_t()
     _check(lib().mkv_beam_workspace(n_batch, n_beams, vocab, n_select, ctypes.byref(n)))

@@ -12,9 +12,16 @@ def _ptr(t):
     return 0 if t is None else int(t.data_ptr())
 
 
+def raw_stream(device):
+    """The current stream of a device as a hipStream_t (torch.cuda.current_stream makes an object first,
+    which takes longer than a launch)."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
 def check_tensor(name, t, device, dtype, shape):
     """A call that reads a device buffer by its pointer needs it to be what the kernels take it for."""
-    if t.device != device or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.device != device or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {device} "
                          f"(got {t.dtype}, {tuple(t.shape)} on {t.device})")
 
@@ -35,6 +42,7 @@ class KVCache:
         self.cfgs = [dict(c) for c in cfgs]
         self.prompt_lens = [int(x) for x in prompt_lens]
         rows = [L.make_config(c) for c in self.cfgs]
+        self._tree_bytes = {}  # nodes -> workspace bytes, which the cache's layout settles
         self.nbytes = L.mkv_cache_bytes(self.shape, rows, self.prompt_lens)
         self.arena = torch.empty(self.nbytes + 256, dtype=torch.uint8, device=device)
         base = self.arena.data_ptr()
@@ -90,9 +98,10 @@ class KVCache:
 
     # ---- drafted trees (mkv_tree_attention, mkv_tree_accept) ----------------------------------
     def tree_workspace(self, n_nodes):
-        """A workspace of tree_attention for n_nodes nodes, for calls that may overlap or be captured."""
-        # (torch aligns an allocation to 512 bytes)
-        return self.torch.empty(L.mkv_tree_workspace(self.h, n_nodes), dtype=self.torch.uint8, device=self.arena.device)
+        """A workspace of tree_attention for n_nodes nodes (torch aligns an allocation to 512 bytes)."""
+        if n_nodes not in self._tree_bytes:
+            self._tree_bytes[n_nodes] = L.mkv_tree_workspace(self.h, n_nodes)
+        return self.torch.empty(self._tree_bytes[n_nodes], dtype=self.torch.uint8, device=self.arena.device)
 
     def tree_attention(self, q, k, v, mask, out=None, n_valid=None, workspace=None):
         """Attention of drafted nodes over the cache and each other -> out [S][N][Hq][D] fp16.
@@ -108,15 +117,22 @@ class KVCache:
         check_tensor("mask", mask, dev, torch.int64, (self.S, n))
         if n_valid is not None:
             check_tensor("n_valid", n_valid, dev, torch.int32, (self.S,))
-        with torch.cuda.stream(self.stream):
-            if out is None:
-                out = torch.empty_like(q)
+        if out is not None:
+            check_tensor("out", out, dev, torch.float16, (self.S, n, self.Hq, self.D))
+        ws = workspace
+        if out is None or ws is None:
+            # memory allocated here belongs to the cache's stream
+            if raw_stream(dev) == self.s:
+                out, ws = self._tree_buffers(q, n, out, ws)
             else:
-                check_tensor("out", out, dev, torch.float16, (self.S, n, self.Hq, self.D))
-            ws = workspace if workspace is not None else self.tree_workspace(n)
-            L.mkv_tree_attention(self.h, _ptr(q), _ptr(k), _ptr(v), _ptr(mask), _ptr(n_valid), n, _ptr(out), _ptr(ws),
-                                 ws.numel(), self.s)
+                with torch.cuda.stream(self.stream):
+                    out, ws = self._tree_buffers(q, n, out, ws)
+        L.mkv_tree_attention(self.h, _ptr(q), _ptr(k), _ptr(v), _ptr(mask), _ptr(n_valid), n, _ptr(out), _ptr(ws),
+                             ws.numel(), self.s)
         return out
+
+    def _tree_buffers(self, q, n, out, ws):
+        return self.torch.empty_like(q) if out is None else out, self.tree_workspace(n) if ws is None else ws
 
     def tree_accept(self, k, v, path, n_path, counts=None):
         """Append nodes path[s][:n_path[s]] of k, v [S][N][Hkv][D] to each sequence; path [S][M], n_path [S]

@@ -348,14 +348,16 @@ struct Rows {
   unsigned long long mask[RB];  // the nodes that the row attends to
 };
 
-// The wave's tokens of a tile in LDS: logits, softmax, output.  Tokens at or past `left` do not exist; TREE:
-// nor does, for a row, a token that its mask does not name.
-template <int D, int RB, int WR, bool TREE>
+// The wave's tokens of a tile in LDS: logits, softmax, output.  References and logits are kept unscaled; the
+// scale (and log2 e) enters with the reference in one fused operation before the exponential.
+// Tokens at or past `left` do not exist; MASKED: nor does, for a row, a token that its mask does not name.
+template <int D, int RB, int WR, bool MASKED>
 MKV_DEV void attend_tile(Tile<D> &t, Rows<D, RB, WR> &x, int left, float qscale) {
   using C = TG<D, RB, WR>;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lq = lane >> 4;
   const int tok0 = (wave % C::WT) * C::TW;
-#pragma unroll
+  const float lazy = kLazy / qscale;
+#pragma unroll 1
   for (int u = 0; u < C::TW / (16 * C::NB); ++u) {
     const int first = tok0 + 16 * C::NB * u;
     f4v S[C::NB][RB];
@@ -371,21 +373,28 @@ MKV_DEV void attend_tile(Tile<D> &t, Rows<D, RB, WR> &x, int left, float qscale)
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) S[b][rb] = mfma32(a, x.q[m][rb], S[b][rb]);
       }
+    if (MASKED || first + 16 * C::NB > left) {
+#pragma unroll
+      for (int b = 0; b < C::NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int token = first + 16 * b + 4 * lq + i;
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb)
+            S[b][rb][i] = token < left && (!MASKED || ((x.mask[rb] >> token) & 1)) ? S[b][rb][i] : -INFINITY;
+        }
+    }
     float mx[RB];
     bool move = false;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       mx[rb] = -INFINITY;
 #pragma unroll
-      for (int b = 0; b < C::NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int token = first + 16 * b + 4 * lq + i;
-          const bool on = token < left && (!TREE || ((x.mask[rb] >> token) & 1));
-          S[b][rb][i] = on ? S[b][rb][i] * qscale : -INFINITY;
-          mx[rb] = fmaxf(mx[rb], S[b][rb][i]);
-        }
-      move |= mx[rb] > x.m[rb] + kLazy;
+      for (int b = 0; b < C::NB; ++b) {
+        mx[rb] = fmaxf(fmaxf(mx[rb], S[b][rb][0]), S[b][rb][1]);
+        mx[rb] = fmaxf(fmaxf(mx[rb], S[b][rb][2]), S[b][rb][3]);
+      }
+      move |= mx[rb] > x.m[rb] + lazy;
     }
     if (__any(move)) {
 #pragma unroll
@@ -393,7 +402,7 @@ MKV_DEV void attend_tile(Tile<D> &t, Rows<D, RB, WR> &x, int left, float qscale)
         float y = fmaxf(mx[rb], __shfl_xor(mx[rb], 16));
         y = fmaxf(y, __shfl_xor(y, 32));
         const bool up = y > x.m[rb];
-        const float corr = up ? fexp2(x.m[rb] - y) : 1.f;
+        const float corr = up ? fexp2((x.m[rb] - y) * qscale) : 1.f;
         if (up) x.m[rb] = y;
         x.l[rb] *= corr;
 #pragma unroll
@@ -402,19 +411,19 @@ MKV_DEV void attend_tile(Tile<D> &t, Rows<D, RB, WR> &x, int left, float qscale)
     }
     uint32_t P[RB][2 * C::NB];
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
+    for (int rb = 0; rb < RB; ++rb) {
+      // (a row that has seen nothing yet has no reference, and only logits of -infinity)
+      const float ref = x.m[rb] == -INFINITY ? 0.f : -x.m[rb] * qscale;
 #pragma unroll
       for (int b = 0; b < C::NB; ++b) {
         float p[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          // (a row that has seen nothing yet has no reference)
-          p[i] = S[b][rb][i] == -INFINITY ? 0.f : fexp2(S[b][rb][i] - x.m[rb]);
-          x.l[rb] += p[i];
-        }
+        for (int i = 0; i < 4; ++i) p[i] = fexp2(__builtin_fmaf(S[b][rb][i], qscale, ref));
+        x.l[rb] += (p[0] + p[1]) + (p[2] + p[3]);
         P[rb][2 * b] = pk_f16(p[0], p[1]);
         P[rb][2 * b + 1] = pk_f16(p[2], p[3]);
       }
+    }
 #pragma unroll
     for (int m = 0; m < C::NM; ++m) {
       const int ch = 16 * m + lr;
@@ -467,7 +476,7 @@ MKV_DEV int64_t first_split(const SeqDesc &sd, int s, const TreeGeo &g) {
 MKV_DEV int tiles_per_split(int n, int splits) { return ((n + kTile - 1) / kTile + 1 + splits - 1) / splits; }
 
 template <int D, int RB, int WR>
-__global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const SeqDesc *__restrict__ seqs,
+__global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(const SeqDesc *__restrict__ seqs,
                                                             const int32_t *__restrict__ state,
                                                             const float *__restrict__ cbtab, TreeArgs a, TreeGeo geo,
                                                             float qscale) {
@@ -505,7 +514,8 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const SeqDesc *__res
       const uint4 u = gld16h(qp + 32 * m + 8 * lq);
       x.q[m][rb] = __builtin_bit_cast(h8v, on ? u : make_uint4(0u, 0u, 0u, 0u));
     }
-    x.mask[rb] = on && tree ? gld(a.mask + (int64_t)s * N + node) : 0ull;
+    // (bits of nodes that do not exist are dropped)
+    x.mask[rb] = on && tree ? gld(a.mask + (int64_t)s * N + node) & (~0ull >> (64 - valid)) : 0ull;
     x.m[rb] = -INFINITY;
     x.l[rb] = 0.f;
 #pragma unroll
@@ -599,6 +609,7 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_attn(const SeqDesc *__res
   for (int rb = 0; rb < RB; ++rb) {
     x.l[rb] += __shfl_xor(x.l[rb], 16);
     x.l[rb] += __shfl_xor(x.l[rb], 32);
+    x.m[rb] *= qscale;  // from here on in log2
   }
   if constexpr (WT > 1) {
     // the waves that share rows: scaled to their common reference, then summed into the first

@@ -6,50 +6,56 @@ current stream of the tensors' device.
 import torch
 
 from . import _lib as L
-from .cache import check_tensor
+from .cache import check_tensor, raw_stream
 
 
-def _rows(name, t, device):
-    if t.device != device or t.dtype != torch.float16 or t.dim() != 3:
-        raise ValueError(f"{name} must be float16 [rows][heads][head_dim] on {device}")
-    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
-        raise ValueError(f"{name}: a row's heads must be contiguous (rows may be any distance apart)")
+def _launch(device, fn, *args):
+    """fn(*args, stream) with the device current and its current stream."""
+    if torch.cuda.current_device() == device.index:
+        fn(*args, raw_stream(device))
+    else:
+        with torch.cuda.device(device):
+            fn(*args, raw_stream(device))
 
 
 def rope(xs, pos, inv_freq, sections=None, layout="halves", inverse=False, out=None):
     """Rotate the rows of each tensor of xs ([rows][heads][head_dim] fp16: a token's queries, its keys)
     by their positions -> a list of outputs.
 
-    pos int32 [axes][rows]; inv_freq float32 [rotary_dim / 2]; sections: frequency pairs per axis
-    (default: all of the one axis); layout "halves" or "pairs"; inverse: turn back (the gradient).
-    out: tensors to write, which may be xs themselves (default: new ones)."""
+    A row's heads are contiguous, the rows at any distance.  pos int32 [axes][rows]; inv_freq float32
+    [rotary_dim / 2]; sections: frequency pairs per axis (default: all of the one axis); layout
+    "halves" or "pairs"; inverse: turn back (the gradient).  out: tensors to write, which may be xs
+    themselves (default: new ones)."""
     dev = xs[0].device
     n_rows, _, d = xs[0].shape
-    sections = [inv_freq.numel()] if sections is None else [int(n) for n in sections]
+    sections = (inv_freq.numel(),) if sections is None else sections
+    pairs = sum(sections)
     check_tensor("pos", pos, dev, torch.int32, (len(sections), n_rows))
-    check_tensor("inv_freq", inv_freq, dev, torch.float32, (sum(sections),))
+    check_tensor("inv_freq", inv_freq, dev, torch.float32, (pairs,))
     if len(sections) > L.ROPE_MAX_AXES:
         raise ValueError(f"at most {L.ROPE_MAX_AXES} axes (got {len(sections)})")
     if layout not in L.ROPE_LAYOUTS:
         raise ValueError(f"layout must be one of {sorted(L.ROPE_LAYOUTS)} (got {layout!r})")
     if out is None:
-        out = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in xs]
+        out = [x.new_empty(x.shape) for x in xs]
     if len(out) != len(xs):
         raise ValueError("out has another number of tensors than xs")
     sets = []
     for x, y in zip(xs, out):
-        _rows("x", x, dev)
-        _rows("out", y, dev)
-        if x.shape != y.shape or x.shape[0] != n_rows or x.shape[2] != d:
-            raise ValueError("xs and out must agree in rows, heads and head_dim")
-        width = x.shape[1] * d
-        # (one row has any stride)
-        sets.append((x.data_ptr(), y.data_ptr(), x.stride(0) if n_rows > 1 else width,
-                     y.stride(0) if n_rows > 1 else width, x.shape[1]))
+        shape, at = x.shape, []
+        if len(shape) != 3 or shape[0] != n_rows or shape[2] != d or y.shape != shape:
+            raise ValueError("xs and out are [rows][heads][head_dim] and agree in rows and head_dim, each pair in heads")
+        width = shape[1] * d
+        for t in (x, y):
+            if t.device != dev or t.dtype != torch.float16:
+                raise ValueError(f"xs and out must be float16 on {dev}")
+            stride = t.stride()
+            if stride[2] != 1 or (shape[1] > 1 and stride[1] != d):
+                raise ValueError("a row's heads must be contiguous (rows may be any distance apart)")
+            at.append(stride[0] if n_rows > 1 else width)  # (one row has any stride)
+        sets.append((x.data_ptr(), y.data_ptr(), at[0], at[1], shape[1]))
     if n_rows > 0:
-        with torch.cuda.device(dev):
-            L.mkv_rope(d, 2 * sum(sections), sections, layout, inv_freq.data_ptr(), pos.data_ptr(), n_rows, sets, inverse,
-                       torch.cuda.current_stream(dev).cuda_stream)
+        _launch(dev, L.mkv_rope, d, 2 * pairs, sections, layout, inv_freq.data_ptr(), pos.data_ptr(), n_rows, sets, inverse)
     return out
 
 
@@ -74,11 +80,9 @@ def beam_select(logits, scores, n_select, finished=None, pad_token=0, workspace=
         check_tensor("finished", finished, dev, torch.uint8, (b, w))
     stride = logits.stride(1) if w > 1 else logits.stride(0) if b > 1 else v
     token = torch.empty((b, n_select), dtype=torch.int32, device=dev)
-    parent, score = torch.empty_like(token), torch.empty((b, n_select), dtype=torch.float32, device=dev)
+    parent, score = torch.empty_like(token), scores.new_empty((b, n_select))
     ws = workspace if workspace is not None else beam_workspace(b, w, v, n_select, dev)
-    with torch.cuda.device(dev):
-        L.mkv_beam_select(logits.data_ptr(), L.F16 if logits.dtype == torch.float16 else L.F32, stride, b, w, v,
-                          scores.data_ptr(), 0 if finished is None else finished.data_ptr(), pad_token, n_select,
-                          token.data_ptr(), parent.data_ptr(), score.data_ptr(), ws.data_ptr(), ws.numel(),
-                          torch.cuda.current_stream(dev).cuda_stream)
+    _launch(dev, L.mkv_beam_select, logits.data_ptr(), L.F16 if logits.dtype == torch.float16 else L.F32, stride, b, w, v,
+            scores.data_ptr(), 0 if finished is None else finished.data_ptr(), pad_token, n_select, token.data_ptr(),
+            parent.data_ptr(), score.data_ptr(), ws.data_ptr(), ws.numel())
     return token, parent, score
