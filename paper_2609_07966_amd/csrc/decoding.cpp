@@ -17,8 +17,8 @@ TreePlan tree_plan(const Shape &sh, const std::vector<SeqDesc> &seqs, int n_node
   const int rows = n_nodes * sh.G;
   p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   p.row_blocks = (rows + p.rows - 1) / p.rows;
-  // two workgroups a CU, all resident at once, by capacity
-  const int64_t target = 2 * kCus;
+  // all workgroups resident at once, by capacity: three a CU of the smaller ones, two of the larger
+  const int64_t target = (p.rows <= 32 ? 3 : 2) * kCus;
   int longest = 0;
   for (const SeqDesc &d : seqs) longest = std::max(longest, d.cap);
   auto count = [&](int chunk) {
@@ -26,7 +26,7 @@ TreePlan tree_plan(const Shape &sh, const std::vector<SeqDesc> &seqs, int n_node
     for (const SeqDesc &d : seqs) n += (d.cap + chunk - 1) / chunk;
     return n * sh.Hkv * p.row_blocks;
   };
-  int lo = 2, hi = std::max(2, (longest + kTreeTile - 1) / kTreeTile);  // tiles
+  int lo = 1, hi = std::max(1, (longest + kTreeTile - 1) / kTreeTile);  // tiles
   while (lo < hi) {
     const int mid = (lo + hi) / 2;
     if (count(mid * kTreeTile) <= target) hi = mid;

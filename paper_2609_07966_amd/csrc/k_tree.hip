@@ -33,6 +33,7 @@ constexpr float kLazy = 2.f;  // the reference of a row's softmax moves when a l
 typedef _Float16 h2v __attribute__((ext_vector_type(2)));
 typedef _Float16 h4v __attribute__((ext_vector_type(4)));
 typedef _Float16 h8v __attribute__((ext_vector_type(8)));
+typedef float f2v __attribute__((ext_vector_type(2)));
 typedef float f4v __attribute__((ext_vector_type(4)));
 
 MKV_DEV f4v mfma32(h8v a, h8v b, f4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -66,6 +67,9 @@ struct Tile {
   uint16_t v[D * kTile];
 };
 MKV_DEV int vswz(int ch) { return (ch ^ (ch >> 3)) & 15; }
+// Byte offset of block b of channel 16 m + lr, given that of m = 0: the swizzle of the channel is that of lr
+// with 2 m xored in, so a read costs one xor (and its 2048 m goes into the instruction).
+MKV_DEV uint32_t v_offset(uint32_t of_lr, int m) { return (of_lr ^ (16 * m & 127)) + 2 * kTile * 16 * m; }
 template <int D>
 MKV_DEV uint16_t *v_at(Tile<D> &t, int ch, int block) { return t.v + ch * kTile + 4 * (block ^ vswz(ch)); }
 template <int D>
@@ -93,6 +97,7 @@ struct RowsLoader {
     uint4 k[NK];
     uint32_t v[4][VPL / 2];
   };
+  MKV_DEV void start(int, Raw &) const {}
   MKV_DEV void fetch(int tile, Raw &r) const {
     const int tid = threadIdx.x, last = n - 1;
 #pragma unroll
@@ -156,6 +161,7 @@ struct UqLoader {
     uint32_t v[NW];  // codes of D / 16 channels x 4 tokens
     float2 vm[4][NGRP];
   };
+  MKV_DEV void start(int, Raw &) const {}
   MKV_DEV void fetch(int tile, Raw &r) const {
     const int tid = threadIdx.x, w = tid % (D / 8);
     const bool whole = (tile + 1) * kTile <= n;
@@ -247,11 +253,21 @@ struct KvqLoader {
   const uint32_t *tau;          // LDS: thresholds of channel pairs
   int n, cap, nov, rowbytes;
   bool outliers;
+  // the tile's range of key outliers, and where its second 32 tokens begin; read one tile ahead of the
+  // entries themselves
+  struct Range {
+    uint32_t e0, emid, e1;
+  };
   struct Raw {
     uint32_t k[BITS], v[BITS];
     float s[4];
-    uint32_t e0, e1, emid;  // the tile's range of key outliers, and where its second 32 tokens begin
+    Range r, next;
+    uint32_t ko, vo;  // this thread's first key and value outlier
   };
+  MKV_DEV Range range(int tile) const {
+    return {gld(krow + min(tile * kTile, n)), gld(krow + min(tile * kTile + 32, n)), gld(krow + min(tile * kTile + 64, n))};
+  }
+  MKV_DEV void start(int tile, Raw &r) const { r.next = range(tile); }
   MKV_DEV void fetch(int tile, Raw &r) const {
     const int tid = threadIdx.x;
     if (UK == kTreeThreads || tid < UK) {
@@ -271,9 +287,11 @@ struct KvqLoader {
       r.s[2] = __builtin_bit_cast(float, s.z);
       r.s[3] = __builtin_bit_cast(float, s.w);
     }
-    r.e0 = gld(krow + tile * kTile);
-    r.emid = gld(krow + min(tile * kTile + 32, n));
-    r.e1 = gld(krow + min(tile * kTile + 64, n));
+    if (!outliers) return;
+    r.r = r.next;
+    if (r.r.e0 + tid < r.r.e1) r.ko = gld(kout + r.r.e0 + tid);
+    if (tid < kTile) r.vo = gld(vout + min(tile * kTile + tid, n - 1));
+    r.next = range(tile + 1);
   }
   // bits [at, at + 2 BITS) of a unit, as the packed pair they stand for
   MKV_DEV uint32_t pair(const uint32_t *lut, const uint32_t (&w)[BITS], int f) const {
@@ -313,19 +331,19 @@ struct KvqLoader {
   }
   MKV_DEV void fix(int tile, const Raw &r, Tile<D> &t) const {
     const int tid = threadIdx.x;
-    for (uint32_t e = r.e0 + tid; e < r.e1; e += kTreeThreads) {
-      const uint32_t x = gld(kout + e);
-      const int token = (outlier_tag(x) & 31) + (e >= r.emid ? 32 : 0);
+    auto key = [&](uint32_t e, uint32_t x) {
+      const int token = (outlier_tag(x) & 31) + (e >= r.r.emid ? 32 : 0);
       t.k[token * Tile<D>::KS + min(outlier_ch(x), D - 1)] = (uint16_t)(x >> 16);
-    }
+    };
+    auto value = [&](int token, uint32_t x) {
+      if (x != kNoOutlier) v_at(t, min(outlier_ch(x), D - 1), token >> 2)[token & 3] = (uint16_t)(x >> 16);
+    };
+    if (r.r.e0 + tid < r.r.e1) key(r.r.e0 + tid, r.ko);
+    for (uint32_t e = r.r.e0 + kTreeThreads + tid; e < r.r.e1; e += kTreeThreads) key(e, gld(kout + e));
     const int left = min(kTile, n - tile * kTile);
-    for (int i = tid; i < kTile * nov; i += kTreeThreads) {
-      const int token = i & 63;
-      if (token >= left) continue;
-      const uint32_t x = gld(vout + (int64_t)(i >> 6) * cap + tile * kTile + token);
-      if (x == kNoOutlier) continue;
-      v_at(t, min(outlier_ch(x), D - 1), token >> 2)[token & 3] = (uint16_t)(x >> 16);
-    }
+    if (tid < left) value(tid, r.vo);
+    for (int i = kTile + tid; i < kTile * nov; i += kTreeThreads)  // (further slots)
+      if ((i & 63) < left) value(i & 63, gld(vout + (int64_t)(i >> 6) * cap + tile * kTile + (i & 63)));
   }
 };
 
@@ -424,12 +442,13 @@ MKV_DEV void attend_tile(Tile<D> &t, Rows<D, RB, WR> &x, int left, float qscale)
         P[rb][2 * b + 1] = pk_f16(p[2], p[3]);
       }
     }
+    const char *vt = reinterpret_cast<const char *>(t.v);
+    const uint32_t v0 = 2 * kTile * lr + 8 * ((first / 4 + lq) ^ vswz(lr));
 #pragma unroll
     for (int m = 0; m < C::NM; ++m) {
-      const int ch = 16 * m + lr;
-      const uint2 a0 = *reinterpret_cast<const uint2 *>(v_at(t, ch, first / 4 + lq));
-      if constexpr (C::NB == 2) {
-        const uint2 a1 = *reinterpret_cast<const uint2 *>(v_at(t, ch, first / 4 + 4 + lq));
+      const uint2 a0 = *reinterpret_cast<const uint2 *>(vt + v_offset(v0, m));
+      if constexpr (C::NB == 2) {  // (first is a multiple of 32 tokens: 4 blocks on is bit 2 of the block)
+        const uint2 a1 = *reinterpret_cast<const uint2 *>(vt + v_offset(v0 ^ 32, m));
         const h8v a = __builtin_bit_cast(h8v, make_uint4(a0.x, a0.y, a1.x, a1.y));
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
@@ -443,10 +462,16 @@ MKV_DEV void attend_tile(Tile<D> &t, Rows<D, RB, WR> &x, int left, float qscale)
   }
 }
 
-template <int D, int RB, int WR, class L>
-MKV_DEV void attend_range(const L &ld, Tile<D> &t, Rows<D, RB, WR> &x, int begin, int end, float qscale) {
+// A wave over tiles [begin, end) of the cache, each tile's loads issued before the one ahead of it is
+// computed; `first()` runs after the first loads are on their way.
+template <int D, int RB, int WR, class L, class F>
+MKV_DEV void attend_range(const L &ld, Tile<D> &t, Rows<D, RB, WR> &x, int begin, int end, float qscale, F first) {
   typename L::Raw raw;
-  if (begin < end) ld.fetch(begin, raw);
+  if (begin < end) {
+    ld.start(begin, raw);
+    ld.fetch(begin, raw);
+  }
+  first();
   for (int tile = begin; tile < end; ++tile) {
     ld.put(tile, raw, t);
     __syncthreads();
@@ -521,13 +546,53 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
 #pragma unroll
     for (int m = 0; m < NM; ++m) x.o[m][rb] = f4v{0.f, 0.f, 0.f, 0.f};
   }
+  // the drafted tokens, whose loads are issued first
+  RowsLoader<D> nodes;
+  nodes.K = a.k + ((int64_t)s * N * geo.Hkv + h) * D;
+  nodes.V = a.v + ((int64_t)s * N * geo.Hkv + h) * D;
+  nodes.stride = (int64_t)geo.Hkv * D;
+  nodes.n = valid;
+  typename RowsLoader<D>::Raw nraw;
+  if (tree) nodes.fetch(0, nraw);
+  auto attend_nodes = [&]() {
+    if (!tree) return;
+    // A value that is infinite or NaN must reach only the rows that attend to its node: it is left out
+    // of the product, where a probability of 0 would make it NaN, and added to those rows.
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const uint32_t w = nraw.v[j][i];
+        const uint32_t bad = ((w & 0x7C00u) == 0x7C00u ? 0xFFFFu : 0u) | ((w & 0x7C000000u) == 0x7C000000u ? 0xFFFF0000u : 0u);
+        odd |= bad != 0u;
+        nraw.v[j][i] = w & ~bad;
+      }
+    nodes.put(0, nraw, tile);
+    const bool any_odd = __syncthreads_or(odd);
+    attend_tile<D, RB, WR, true>(tile, x, valid, qscale);
+    if (any_odd && wt == 0) {
+      for (int j = 0; j < valid; ++j)
+#pragma unroll
+        for (int m = 0; m < NM; ++m)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w = gld(nodes.V + j * nodes.stride + 16 * m + 4 * lq + i);
+            if ((w & 0x7C00u) != 0x7C00u) continue;
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+              if ((x.mask[rb] >> j) & 1) x.o[m][rb][i] += h2f(w);
+          }
+    }
+    __syncthreads();
+  };
   if (sd.method == FP16) {
     RowsLoader<D> ld;
     ld.K = reinterpret_cast<const uint16_t *>(sd.k) + h * stride_rows(sd, D);
     ld.V = reinterpret_cast<const uint16_t *>(sd.v) + h * stride_rows(sd, D);
     ld.stride = D;
     ld.n = n;
-    attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale);
+    attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale, attend_nodes);
   } else if (sd.method == UQ) {
     UqLoader<D> ld;
     ld.kc = reinterpret_cast<const uint8_t *>(sd.kc) + h * stride_codes(sd);
@@ -536,7 +601,7 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
     ld.vmeta = reinterpret_cast<const float *>(sd.vmeta) + h * stride_uq_vmeta(sd, D) * 2;
     ld.kres = reinterpret_cast<const uint16_t *>(sd.kres) + (int64_t)h * kTile * D;
     ld.n = n;
-    attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale);
+    attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale, attend_nodes);
   } else {
     auto run = [&](auto bits_tag) {
       constexpr int BITS = decltype(bits_tag)::value;
@@ -560,49 +625,11 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
       ld.nov = sd.nov_slots;
       ld.rowbytes = sd.rowbytes;
       ld.outliers = sd.bp > 0;
-      attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale);
+      attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale, attend_nodes);
     };
     if (sd.bits == 4) run(std::integral_constant<int, 4>{});
     else if (sd.bits == 3) run(std::integral_constant<int, 3>{});
     else run(std::integral_constant<int, 2>{});
-  }
-  if (tree) {
-    RowsLoader<D> ld;
-    ld.K = a.k + ((int64_t)s * N * geo.Hkv + h) * D;
-    ld.V = a.v + ((int64_t)s * N * geo.Hkv + h) * D;
-    ld.stride = (int64_t)geo.Hkv * D;
-    ld.n = valid;
-    typename RowsLoader<D>::Raw raw;
-    ld.fetch(0, raw);
-    // A value that is infinite or NaN must reach only the rows that attend to its node: it is left out
-    // of the product, where a probability of 0 would make it NaN, and added to those rows.
-    bool odd = false;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        const uint32_t w = raw.v[j][i];
-        const uint32_t bad = ((w & 0x7C00u) == 0x7C00u ? 0xFFFFu : 0u) | ((w & 0x7C000000u) == 0x7C000000u ? 0xFFFF0000u : 0u);
-        odd |= bad != 0u;
-        raw.v[j][i] = w & ~bad;
-      }
-    ld.put(0, raw, tile);
-    const bool any_odd = __syncthreads_or(odd);
-    attend_tile<D, RB, WR, true>(tile, x, valid, qscale);
-    if (any_odd && wt == 0) {
-      for (int j = 0; j < valid; ++j)
-#pragma unroll
-        for (int m = 0; m < NM; ++m)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t w = gld(ld.V + j * ld.stride + 16 * m + 4 * lq + i);
-            if ((w & 0x7C00u) != 0x7C00u) continue;
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-              if ((x.mask[rb] >> j) & 1) x.o[m][rb][i] += h2f(w);
-          }
-    }
-    __syncthreads();
   }
   // a row's four quads hold disjoint tokens
 #pragma unroll
@@ -678,12 +705,12 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
     const int row = (wr * RB + rb) * 16 + lr;
 #pragma unroll
     for (int m = 0; m < NM; ++m) gst(reinterpret_cast<f4v *>(part + row * D + 16 * m + 4 * lq), x.o[m][rb]);
-    if (lq == 0) gst(reinterpret_cast<u32x2 *>(part + R * D + row * 2),
-                     u32x2{__builtin_bit_cast(uint32_t, x.m[rb]), __builtin_bit_cast(uint32_t, x.l[rb])});
+    if (lq == 0) gst(reinterpret_cast<f2v *>(part + R * D + row * 2), f2v{x.m[rb], x.l[rb]});
   }
 }
 
-// Merge of the splits: a thread takes 4 channels of a row.
+// Merge of the splits: a thread takes 4 channels of a row, the loads of 8 splits at a time.
+constexpr int kMergeLoads = 8;
 template <int D>
 __global__ __launch_bounds__(256) void k_tree_merge(const SeqDesc *__restrict__ seqs, const int32_t *__restrict__ state,
                                                     TreeArgs a, TreeGeo geo, int R) {
@@ -701,16 +728,32 @@ __global__ __launch_bounds__(256) void k_tree_merge(const SeqDesc *__restrict__ 
   const int64_t step = (int64_t)geo.Hkv * geo.row_blocks * R * (D + 2);
   const float *part = a.workspace + ((first_split(sd, s, geo) * geo.Hkv + h) * geo.row_blocks + row / R) * (int64_t)(R * (D + 2));
   const float *ml = part + R * D + (row % R) * 2, *o = part + (row % R) * D + c;
-  float M = -INFINITY;
-  for (int p = 0; p < used; ++p) M = fmaxf(M, gld(ml + p * step));
-  float Ls = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < used; ++p) {
-    const float m = gld(ml + p * step), l = gld(ml + p * step + 1);
-    const f4v v = gld(reinterpret_cast<const f4v *>(o + p * step));
-    const float w = m == -INFINITY ? 0.f : fexp2(m - M);
-    Ls += l * w;
+  float M = -INFINITY, Ls = 0.f;
+  f4v acc = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = 0; p0 < used; p0 += kMergeLoads) {
+    f2v x[kMergeLoads];  // (maximum, sum)
+    f4v v[kMergeLoads];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] += m == -INFINITY ? 0.f : v[i] * w;
+    for (int i = 0; i < kMergeLoads; ++i) {
+      const int64_t at = min(p0 + i, used - 1) * step;
+      x[i] = gld(reinterpret_cast<const f2v *>(ml + at));
+      v[i] = gld(reinterpret_cast<const f4v *>(o + at));
+    }
+    float top = M;
+#pragma unroll
+    for (int i = 0; i < kMergeLoads; ++i) top = fmaxf(top, x[i][0]);
+    const float old = M == -INFINITY ? 0.f : fexp2(M - top);
+    Ls *= old;
+    acc *= old;
+    M = top;
+#pragma unroll
+    for (int i = 0; i < kMergeLoads; ++i) {
+      const float m = x[i][0];
+      if (p0 + i >= used || m == -INFINITY) continue;
+      const float w = fexp2(m - M);
+      Ls += x[i][1] * w;
+      acc += v[i] * w;
+    }
   }
   uint16_t *op = a.out + (((int64_t)s * N + node) * Hq + h * G + row % G) * D + c;
   const float inv = 1.f / Ls;
@@ -746,34 +789,234 @@ hipError_t tree_rows(const Dev &dv, const Shape &sh, const TreePlan &plan, const
 }
 
 // ---- acceptance -----------------------------------------------------------------------------------------
-// One workgroup of D threads per (sequence, kv head) appends the path's tokens one after another (a token's
-// place among the outliers, its 4-token value block and its key block depend on the ones before).
+// One workgroup per (sequence, kv head), a wave per token and 8 tokens at a time: each wave quantizes its
+// token by itself (D / 64 channels a lane, reductions and ranks over the wave, no barriers), with the same
+// rounded float32 steps as the decode append (append_dev.h), whose codes it gives bit for bit.  What a token
+// needs of the ones before it: its place among the key outliers, from the waves' counts; the 4-token value
+// blocks, put together in LDS; the rows of a uniform 4-bit key block, which ends a group of tokens.
+// Bound by latency: two round trips and two barriers a group (8 tokens of KVQuant 4-bit one after another
+// by the append's workgroup of D threads take 33 us, so 5).
+constexpr int kAcceptWaves = 8;
+
 template <int D>
-__global__ __launch_bounds__(D) void k_tree_accept(const SeqDesc *__restrict__ seqs, int32_t *state,
-                                                   const uint16_t *__restrict__ k, const uint16_t *__restrict__ v,
-                                                   const float *__restrict__ cbtab, int Hkv, int n_nodes,
-                                                   const int32_t *__restrict__ path, const int32_t *__restrict__ n_path,
-                                                   int max_path, int32_t *counts) {
-  __shared__ AppendLds<D> L;
-  const int seq = blockIdx.x / Hkv, h = blockIdx.x % Hkv;
+struct AcceptLds {
+  float mid[2][16];                  // KVQ: midpoints of the key and of the value codebook, then infinity
+  float cbv[16];                     // KVQ: value codebook
+  float abs[kAcceptWaves][D];        // KVQ, several value outliers a token
+  uint32_t row[kAcceptWaves][D / 8]; // a token's packed key codes
+  uint32_t blk[3][D / 2];            // value codes of the group's 4-token blocks
+  int outliers[kAcceptWaves];
+  int take;
+};
+
+template <int D>
+__global__ __launch_bounds__(64 * kAcceptWaves) void k_tree_accept(const SeqDesc *__restrict__ seqs, int32_t *state,
+                                                                   const uint16_t *__restrict__ k,
+                                                                   const uint16_t *__restrict__ v,
+                                                                   const float *__restrict__ cbtab, int Hkv, int n_nodes,
+                                                                   const int32_t *__restrict__ path,
+                                                                   const int32_t *__restrict__ n_path, int max_path,
+                                                                   int32_t *counts) {
+  constexpr int CH = D / 64, NT = 64 * kAcceptWaves;
+  __shared__ AcceptLds<D> L;
+  const int seq = blockIdx.x / Hkv, h = blockIdx.x % Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const SeqDesc &sd = seqs[seq];
   int32_t *st = state + ((int64_t)seq * Hkv + h) * ST_WORDS;
-  int count = st[ST_COUNT], pos = st[ST_NEXT_POS];
-  const int take = min(max(n_path[seq], 0), max_path);
-  for (int i = 0; i < take; ++i) {
-    const int node = path[(int64_t)seq * max_path + i];
-    if (node < 0 || node >= n_nodes) break;
-    // load_token reads row `seq` of its k and v: the node's row is (seq (n_nodes - 1) + node) further
-    const int64_t ahead = ((int64_t)seq * (n_nodes - 1) + node) * Hkv * D;
-    const NewToken tok = load_token<D, D>(sd, st, seq, h, Hkv, k + ahead, v + ahead, cbtab, L);
-    if (!append_pair<D, D>(sd, st, tok, h, count, pos, count, -1, L)) break;
-    ++count;
-    ++pos;
-    // the next token reads what this one wrote (state, value block, key rows)
-    __builtin_amdgcn_s_waitcnt(0);
+  const int32_t *nodes = path + (int64_t)seq * max_path;
+  const int method = sd.method, bits = sd.bits, cap = sd.cap;
+  int count = st[ST_COUNT], pos = st[ST_NEXT_POS], fill = st[ST_KOUT_FILL];
+  const int want = min(max(n_path[seq], 0), max_path);
+  if (tid == 0) L.take = want;
+  __syncthreads();
+  for (int i = tid; i < want; i += NT)
+    if (nodes[i] < 0 || nodes[i] >= n_nodes) atomicMin(&L.take, i);
+  const int words = method == UQ ? D / 2 : method == KVQ ? D * bits / 8 : 0;  // of a value block
+  uint32_t *blocks = reinterpret_cast<uint32_t *>(reinterpret_cast<uint8_t *>(sd.vc) + h * stride_codes(sd));
+  for (int i = tid; i < 3 * (D / 2); i += NT) L.blk[i / (D / 2)][i % (D / 2)] = 0u;
+  if (method == KVQ && tid < 48) {
+    const int nc = 1 << bits, i = tid & 15;
+    const float *cb = cbtab + cb_offset(bits);
+    if (tid < 32) L.mid[tid >> 4][i] = i < nc - 1 ? cb[2 * nc + (tid >> 4) * (nc - 1) + i] : INFINITY;
+    else L.cbv[i] = i < nc ? cb[nc + i] : 0.f;
+  }
+  __syncthreads();
+  // the open value block goes on (its words by the threads that store them below)
+  if (tid < words && (count & 3) != 0) L.blk[0][tid] = gld(blocks + (int64_t)(count >> 2) * words + tid);
+  const int take = min(L.take, cap - count);
+  float2 tau[CH];
+#pragma unroll
+  for (int i = 0; i < CH; ++i) tau[i] = method == KVQ ? kvq_key_tau(sd, h, lane + 64 * i, D) : make_float2(0.f, 0.f);
+  auto code_of = [&](float x, const float *mid) {
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < 15; ++i) c += x > mid[i] ? 1 : 0;
+    return c;
+  };
+  auto before = [&](uint64_t m) { return __popcll(m & ((1ull << lane) - 1)); };
+  __syncthreads();
+  for (int done = 0; done < take;) {
+    // the tokens of this group: up to the end of a key block, and as many as the key-outlier pool has room
+    // for whatever they hold (a token that may not fit is dropped, as by the decode append)
+    int m = min(kAcceptWaves, take - done);
+    if (method == UQ) m = min(m, 64 - (count & 63));
+    if (method == KVQ && sd.bp > 0) {
+      if (fill + D > sd.pool_cap) break;
+      m = min(m, (sd.pool_cap - fill) / D);
+    }
+    const int t = count + wave;
+    const bool on = wave < m;
+    uint32_t kx[CH], vx[CH];
+    int kcode[CH];
+    uint64_t kout[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) kx[i] = vx[i] = 0, kcode[i] = 0, kout[i] = 0;
+    if (on) {
+      const int64_t at = (((int64_t)seq * n_nodes + nodes[done + wave]) * Hkv + h) * D + lane;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        kx[i] = gld(k + at + 64 * i);
+        vx[i] = gld(v + at + 64 * i);
+      }
+      uint32_t *blk = L.blk[(t >> 2) - (count >> 2)];
+      if (method == FP16) {
+        uint16_t *kr = reinterpret_cast<uint16_t *>(sd.k) + h * stride_rows(sd, D) + (int64_t)t * D + lane;
+        uint16_t *vr = reinterpret_cast<uint16_t *>(sd.v) + h * stride_rows(sd, D) + (int64_t)t * D + lane;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+          gst(kr + 64 * i, (uint16_t)kx[i]);
+          gst(vr + 64 * i, (uint16_t)vx[i]);
+        }
+      } else if (method == UQ) {
+        uint16_t *res = reinterpret_cast<uint16_t *>(sd.kres) + ((int64_t)h * 64 + (t & 63)) * D + lane;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {  // a lane's channels are one of each value group
+          gst(res + 64 * i, (uint16_t)kx[i]);
+          const float x = h2f(vx[i]), mn = wave_min(x), mx = wave_max(x), r = __fsub_rn(mx, mn);
+          const float inv = r > 0.f ? __fdiv_rn(15.0f, r) : 0.f;
+          const int code = (int)fminf(fmaxf(rintf(__fmul_rn(__fsub_rn(x, mn), inv)), 0.f), 15.f);
+          or_uq_code(blk, lane + 64 * i, t & 3, code, D);
+          if (lane == 0)
+            (reinterpret_cast<float2 *>(sd.vmeta) + h * stride_uq_vmeta(sd, D))[(int64_t)t * CH + i] = make_float2(mn, __fdiv_rn(r, 15.0f));
+        }
+      } else {
+        // key: codes under the frozen thresholds, packed; outliers wait for their place
+        uint32_t *row = L.row[wave];
+        if (lane < D / 8) row[lane] = 0u;
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+          const float x = h2f(kx[i]);
+          kcode[i] = code_of(__fmul_rn(x, tau[i].y), L.mid[0]);
+          kout[i] = __ballot(sd.bp > 0 && fabsf(x) > tau[i].x);
+          const int bit = bits * (lane + 64 * i);
+          atomicOr(&row[bit >> 5], (uint32_t)kcode[i] << (bit & 31));
+          if ((bit & 31) + bits > 32) atomicOr(&row[(bit >> 5) + 1], (uint32_t)kcode[i] >> (32 - (bit & 31)));
+        }
+        // value: the scale is the n_ov-th largest magnitude (0-based)
+        const int nov = sd.bp > 0 ? sd.n_ov : 0;
+        float ax[CH], s;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) ax[i] = fabsf(h2f(vx[i]));
+        if (nov <= 1) {
+          s = wave_max(CH == 2 ? fmaxf(ax[0], ax[CH - 1]) : ax[0]);
+          int ties = 0;
+          float lower = -1.f;
+#pragma unroll
+          for (int i = 0; i < CH; ++i) {
+            ties += __popcll(__ballot(ax[i] == s));
+            lower = fmaxf(lower, ax[i] < s ? ax[i] : -1.f);
+          }
+          if (nov == 1 && ties < 2) s = wave_max(lower);
+        } else {
+          float *all = L.abs[wave];
+#pragma unroll
+          for (int i = 0; i < CH; ++i) all[lane + 64 * i] = ax[i];
+          __builtin_amdgcn_wave_barrier();
+          s = 0.f;
+#pragma unroll
+          for (int i = 0; i < CH; ++i) {
+            int gt = 0, ge = 0;
+            for (int j = 0; j < D; ++j) {
+              gt += all[j] > ax[i] ? 1 : 0;
+              ge += all[j] >= ax[i] ? 1 : 0;
+            }
+            const uint64_t hit = __ballot(gt <= nov && nov < ge);  // (every hit holds the same value)
+            if (hit) s = __shfl(ax[i], __builtin_ctzll(hit));
+          }
+        }
+        const float inv = s > 0.f ? __fdiv_rn(1.0f, s) : 0.f;
+        uint32_t *vo = reinterpret_cast<uint32_t *>(sd.vout) + h * stride_vout(sd) + t;
+        uint32_t *vd = reinterpret_cast<uint32_t *>(sd.vdel) + h * stride_vout(sd) + t;
+        int total = 0;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+          const float x = h2f(vx[i]);
+          const int code = code_of(__fmul_rn(x, inv), L.mid[1]), c = lane + 64 * i;
+          or_quad_code(blk, c, t & 3, code, bits);
+          const uint64_t out = __ballot(sd.bp > 0 && ax[i] > s);
+          const int r = total + before(out);
+          if ((out >> lane & 1) && r < sd.nov_slots) {
+            gst(vo + (int64_t)r * cap, outlier_entry(vx[i], t, code, c));
+            gst(vd + (int64_t)r * cap, vdel_pack(__fsub_rn(x, __fmul_rn(s, L.cbv[code])), c));
+          }
+          total += __popcll(out);
+        }
+        for (int r = total + lane; r < sd.nov_slots; r += 64) {
+          gst(vo + (int64_t)r * cap, kNoOutlier);
+          gst(vd + (int64_t)r * cap, 0u);
+        }
+        if (lane == 0) gst(reinterpret_cast<float *>(sd.vmeta) + h * stride_slots(sd) + t, s);
+        __builtin_amdgcn_wave_barrier();
+        if (lane < D * bits / 32)
+          gst(reinterpret_cast<uint32_t *>(reinterpret_cast<uint8_t *>(sd.kc) + h * stride_codes(sd) + (int64_t)t * sd.rowbytes) + lane,
+              row[lane]);
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) n += __popcll(kout[i]);
+        if (lane == 0) L.outliers[wave] = n;
+      }
+    }
+    if (method == UQ) __builtin_amdgcn_s_waitcnt(0);  // the key rows, before other waves read them
+    __syncthreads();
+    if (method == KVQ) {
+      int at = fill;
+      for (int w = 0; w < m; ++w) {
+        fill += L.outliers[w];
+        at += w < wave ? L.outliers[w] : 0;
+      }
+      if (on) {
+        uint32_t *pool = reinterpret_cast<uint32_t *>(sd.kout) + h * stride_kout(sd);
+        int r = at;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+          if (kout[i] >> lane & 1) gst(pool + r + before(kout[i]), outlier_entry(kx[i], t, kcode[i], lane + 64 * i));
+          r += __popcll(kout[i]);
+        }
+        if (lane == 0) gst(reinterpret_cast<uint32_t *>(sd.krow) + h * stride_krow(sd) + t + 1, (uint32_t)r);
+      }
+    }
+    const int first = count >> 2, last = (count + m - 1) >> 2;
+    if (tid < words) {
+      uint32_t open = 0u;  // what the next group's first block goes on from
+      for (int b = first; b <= last; ++b) {
+        open = L.blk[b - first][tid];
+        gst(blocks + (int64_t)b * words + tid, open);
+        L.blk[b - first][tid] = 0u;
+      }
+      if (((count + m) & 3) != 0) L.blk[0][tid] = open;
+    }
+    count += m;
+    pos += m;
+    done += m;
+    if (method == UQ && (count & 63) == 0 && tid < D) {
+      // a complete key block: thread c quantizes channel c
+      const uint16_t *res = reinterpret_cast<const uint16_t *>(sd.kres) + (int64_t)h * 64 * D + tid;
+      uq_key_block<D>(sd, h, (count >> 6) - 1, [&](int j) { return (uint32_t)gld(res + j * D); });
+    }
     __syncthreads();
   }
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
+    st[ST_KOUT_FILL] = fill;
     set_counts(st, count, pos);
     if (counts != nullptr && h == 0) counts[seq] = count;
   }
@@ -788,7 +1031,7 @@ hipError_t launch_tree_attention(const Dev &dv, const Shape &sh, const TreePlan 
 hipError_t launch_tree_accept(const Dev &dv, const Shape &sh, const uint16_t *k, const uint16_t *v, int n_nodes,
                               const int32_t *path, const int32_t *n_path, int max_path, int32_t *counts, hipStream_t st) {
   auto kernel = sh.D == 64 ? k_tree_accept<64> : k_tree_accept<128>;
-  hipLaunchKernelGGL(kernel, dim3(sh.S * sh.Hkv), dim3(sh.D), 0, st, dv.seqs, dv.state, k, v, dv.cbtab, sh.Hkv, n_nodes,
+  hipLaunchKernelGGL(kernel, dim3(sh.S * sh.Hkv), dim3(64 * kAcceptWaves), 0, st, dv.seqs, dv.state, k, v, dv.cbtab, sh.Hkv, n_nodes,
                      path, n_path, max_path, counts);
   return hipGetLastError();
 }
