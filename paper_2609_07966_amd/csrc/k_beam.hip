@@ -7,12 +7,11 @@
 // in float64 (two beams' scores lie closer than float32 tells apart once in some thousand selections).
 // Bound by reading the logits once.
 //
-// Choosing the best K of a workgroup's values: every value has a unique 64-bit key (order-preserving
-// bits of the value, then the lower index first).  The keys' maxima over groups of 16 lanes are 64 keys
-// of the workgroup, and the K-th largest of these (K <= 64) is not above the K-th largest key of
-// all: only the values that reach it (about K of random ones, at most the values of K groups) are
-// collected and ranked against each other.  Where they do not fit the list (values in ascending order, or
-// constant), the best ones are taken one after another.
+// Choosing the best K of a workgroup's values: the maxima over groups of 16 lanes are 64 values, and the
+// K-th largest of these (K <= 64) is not above the K-th largest of all.  Only the values that reach it are
+// collected (about K of random ones), as unique 64-bit keys (order-preserving bits of the value, then the
+// lower index first), and ranked against each other.  Where they do not fit the list (values in ascending
+// order, or constant), the best ones are taken one after another.
 #include <algorithm>
 
 #include "kernels_common.h"
@@ -29,13 +28,19 @@ static_assert(2 * MKV_BEAM_MAX <= kBeamGroups && kBeamGroups == 64, "the K-th la
 
 typedef unsigned long long u64;
 
-// Largest key over each row of 16 lanes, in all its lanes.
+// Largest value over each row of 16 lanes, in all its lanes.
+template <int CTRL>
+MKV_DEV uint32_t dpp_u32(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false); }
+MKV_DEV uint32_t row_max_u32(uint32_t x) {
+  x = max(x, dpp_u32<0xB1>(x));
+  x = max(x, dpp_u32<0x4E>(x));
+  x = max(x, dpp_u32<0x141>(x));
+  return max(x, dpp_u32<0x140>(x));
+}
 MKV_DEV u64 row_max_u64(u64 x) {
   auto step = [&](auto ctrl) {
     constexpr int C = decltype(ctrl)::value;
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, C, 0xF, 0xF, false);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), C, 0xF, 0xF, false);
-    const u64 y = ((u64)hi << 32) | lo;
+    const u64 y = ((u64)dpp_u32<C>((uint32_t)(x >> 32)) << 32) | dpp_u32<C>((uint32_t)x);
     x = y > x ? y : x;
   };
   step(std::integral_constant<int, 0xB1>{});
@@ -45,22 +50,24 @@ MKV_DEV u64 row_max_u64(u64 x) {
   return x;
 }
 
-// The K-th largest of the 64 values in `s` (by lane order among equals), for one whole wave.
-MKV_DEV u64 kth_of_64(const u64 *s, int k) {
+// The K-th largest of the 64 values in `s` (16-byte aligned), for one whole wave.
+MKV_DEV uint32_t kth_of_64(const uint32_t *s, int k) {
   const int lane = threadIdx.x & 63;
-  const u64 mine = s[lane];
-  int above = 0;
-  for (int i = 0; i < 64; ++i) {
-    const u64 o = s[i];
-    above += (o > mine || (o == mine && i < lane)) ? 1 : 0;
+  const uint32_t mine = s[lane];
+  int above = 0, reach = 0;  // values over this one; values not under it
+#pragma unroll
+  for (int i = 0; i < 64; i += 4) {
+    const uint4 o = *reinterpret_cast<const uint4 *>(s + i);
+    above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+    reach += (o.x >= mine) + (o.y >= mine) + (o.z >= mine) + (o.w >= mine);
   }
-  const u64 hit = __ballot(above == k - 1);  // exactly one lane
-  return s[__builtin_ctzll(hit)];
+  return s[__builtin_ctzll(__ballot(above < k && reach >= k))];
 }
 
 struct PickLds {
-  u64 group[kBeamGroups];
-  u64 tau;
+  __attribute__((aligned(16))) uint32_t group[kBeamGroups];
+  u64 group64[kBeamGroups];  // where the list overflows
+  uint32_t tau;
   int n;
 };
 
@@ -113,17 +120,13 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_scan(const T *__restrict_
     }
   }
   float mx = -INFINITY;
-  u64 best = 0;
   auto key_of = [&](int i, float v) { return chunk_key(v, base + ((i >> 2) * kBeamThreads + tid) * 4 + (i & 3)); };
 #pragma unroll
   for (int i = 0; i < E; ++i) {
     if (!(x[i] > -INFINITY)) x[i] = -INFINITY;  // NaN
     mx = fmaxf(mx, x[i]);
   }
-#pragma unroll
-  for (int i = E - 1; i >= 0; --i) best = x[i] == mx ? key_of(i, x[i]) : best;  // the lowest index of the maximum
-  if (mx == -INFINITY) best = 0;
-  const u64 gm = row_max_u64(best);
+  const uint32_t gm = row_max_u32(float_key(mx));
   if ((lane & 15) == 0) L.group[tid >> 4] = gm;
   const float wm = wave_max(mx);
   if (lane == 0) s_max[wave] = wm;
@@ -133,7 +136,7 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_scan(const T *__restrict_
 #pragma unroll
   for (int w = 1; w < kBeamWaves; ++w) M = fmaxf(M, s_max[w]);
   if (wave == 0) {
-    const u64 t = kth_of_64(L.group, k);
+    const uint32_t t = kth_of_64(L.group, k);
     if (lane == 0) L.tau = t;
   }
   // the sum of exponentials: float32 over a thread's values, float64 over the threads
@@ -147,14 +150,13 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_scan(const T *__restrict_
   for (int m = 32; m >= 1; m >>= 1) ds += __shfl_xor(ds, m);
   if (lane == 0) s_sum[wave] = ds;
   __syncthreads();
-  const u64 tau = L.tau;
+  const uint32_t tau = max(L.tau, float_key(-INFINITY) + 1u);
+  if (float_key(mx) >= tau) {
 #pragma unroll
-  for (int i = 0; i < E; ++i) {
-    if (x[i] == -INFINITY) continue;
-    const u64 key = key_of(i, x[i]);
-    if (key >= tau) {
+    for (int i = 0; i < E; ++i) {
+      if (float_key(x[i]) < tau) continue;
       const int at = atomicAdd(&L.n, 1);
-      if (at < kListCap) s_list[at] = key;
+      if (at < kListCap) s_list[at] = key_of(i, x[i]);
     }
   }
   __syncthreads();
@@ -184,10 +186,10 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_scan(const T *__restrict_
       }
       const u64 g = row_max_u64(top);
       __syncthreads();
-      if ((lane & 15) == 0) L.group[tid >> 4] = g;
+      if ((lane & 15) == 0) L.group64[tid >> 4] = g;
       __syncthreads();
       u64 all = 0;
-      for (int i = 0; i < kBeamGroups; ++i) all = L.group[i] > all ? L.group[i] : all;
+      for (int i = 0; i < kBeamGroups; ++i) all = L.group64[i] > all ? L.group64[i] : all;
       last = all;  // (n > kListCap >= k values are there)
       if (tid == 0) {
         const uint32_t o = (uint32_t)(all >> 32);
@@ -231,11 +233,23 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_merge(BeamArgs a, const B
   __shared__ int s_done[MKV_BEAM_MAX];
   __shared__ Rank s_group[kBeamGroups];
   __shared__ Rank s_list[kListCap / 2];
-  __shared__ Rank s_tau;
+  __shared__ __attribute__((aligned(16))) uint32_t s_group32[kBeamGroups];
+  __shared__ uint32_t s_tau;
   __shared__ int s_n;
   constexpr int kCap = kListCap / 2;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int b = blockIdx.x, W = a.n_beams, K = a.n_select;
+  const int per = n_chunks * K, total = W * per;
+  auto cand_of = [&](int i) { return cands[(int64_t)b * total + i]; };
+  // (the thread's first candidate is on its way while the beams' sums are put together)
+  const BeamCandidate mine = cand_of(min(tid, total - 1));
+  auto rank = [&](int i, const BeamCandidate &c) {
+    const int w = i / per;
+    if (s_done[w])
+      return i % per == 0 ? Rank{double_key(s_base[w]), (u64)w * a.vocab + a.pad_token} : Rank{0, ~0ull};
+    if (c.token < 0) return Rank{0, ~0ull};
+    return Rank{double_key(s_base[w] + (double)c.logit), (u64)w * a.vocab + c.token};
+  };
   if (tid == 0) s_n = 0;
   for (int w = wave; w < W; w += kBeamWaves) {
     const int64_t row = (int64_t)b * W + w;
@@ -257,41 +271,32 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_merge(BeamArgs a, const B
   }
   __syncthreads();
   // candidate i: beam i / per, the i % per-th of its chunks' candidates
-  const int per = n_chunks * K, total = W * per;
-  auto rank_of = [&](int i) {
-    const int w = i / per, j = i % per;
-    if (s_done[w])
-      return j == 0 ? Rank{double_key(s_base[w]), (u64)w * a.vocab + a.pad_token} : Rank{0, ~0ull};
-    const BeamCandidate c = cands[((int64_t)b * W + w) * per + j];
-    if (c.token < 0) return Rank{0, ~0ull};
-    return Rank{double_key(s_base[w] + (double)c.logit), (u64)w * a.vocab + c.token};
-  };
+  auto rank_of = [&](int i) { return rank(i, cand_of(i)); };
   Rank best = {0, ~0ull};
-  for (int i = tid; i < total; i += kBeamThreads) {
+  if (tid < total) best = rank(tid, mine);
+  for (int i = tid + kBeamThreads; i < total; i += kBeamThreads) {
     const Rank r = rank_of(i);
     if (above(r, best)) best = r;
   }
-  best = row_best(best);
-  if ((lane & 15) == 0) s_group[tid >> 4] = best;
+  const Rank first = total <= kBeamThreads ? best : tid < total ? rank(tid, mine) : Rank{0, ~0ull};
+  // the K-th best group by the upper half of its score
+  const uint32_t gm = row_max_u32((uint32_t)(best.score >> 32));
+  if ((lane & 15) == 0) s_group32[tid >> 4] = gm;
   __syncthreads();
-  if (wave == 0) {  // the K-th best group
-    const Rank mine = s_group[lane];
-    int n = 0;
-    for (int i = 0; i < kBeamGroups; ++i) {
-      const Rank o = s_group[i];
-      n += above(o, mine) || (o.score == mine.score && o.index == mine.index && i < lane) ? 1 : 0;
-    }
-    if (n == K - 1) s_tau = mine;
+  if (wave == 0) {
+    const uint32_t t = kth_of_64(s_group32, K);
+    if (lane == 0) s_tau = t;
   }
   __syncthreads();
-  const Rank tau = s_tau;
-  for (int i = tid; i < total; i += kBeamThreads) {
-    const Rank r = rank_of(i);
-    if (r.score != 0 && !above(tau, r)) {
-      const int at = atomicAdd(&s_n, 1);
-      if (at < kCap) s_list[at] = r;
-    }
-  }
+  const uint32_t tau = s_tau;
+  auto collect = [&](const Rank &r) {
+    if (r.score == 0 || (uint32_t)(r.score >> 32) < tau) return;
+    const int at = atomicAdd(&s_n, 1);
+    if (at < kCap) s_list[at] = r;
+  };
+  collect(first);
+  if ((uint32_t)(best.score >> 32) >= tau)
+    for (int i = tid + kBeamThreads; i < total; i += kBeamThreads) collect(rank_of(i));
   __syncthreads();
   const int n = s_n;
   auto write = [&](int at, const Rank &r) {

@@ -81,15 +81,19 @@ MKV_DEV void put_k8(Tile<D> &t, int token, int ch, const uint32_t *w) {
   *reinterpret_cast<uint4 *>(t.k + token * Tile<D>::KS + ch) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// ---- tile loaders: fetch(tile, raw) reads a tile's data into registers, put(tile, raw, lds) writes it as
-// fp16 rows, fix(tile, raw, lds) (after a barrier; kFix) writes what replaces some of them.  Tokens at or
-// past `n` get value rows of zero (their probabilities are 0, and 0 x anything must stay 0).
+// ---- tile loaders: fetch(tile, raw, carry) reads a tile's data into registers, kDepth tiles ahead of
+// put(tile, raw, lds), which writes it as fp16 rows; fix(tile, raw, lds) (kFix, after a barrier) writes what
+// replaces some of them.  Tokens at or past `n` get value rows of zero (their probabilities are 0, and 0 x
+// anything must stay 0).  A quantized tile is a quarter of the bytes of fp16 rows, so more of them have to
+// be on their way to cover the memory's latency.
 
 // fp16 rows `stride` elements apart: a cache's, or the drafted ones
 template <int D>
 struct RowsLoader {
   static constexpr bool kFix = false;
+  static constexpr int kDepth = 1;
   static constexpr int NK = D / 32, VPL = D / 16;  // key pieces, value channels per thread
+  struct Carry {};
   const uint16_t *K, *V;
   int64_t stride;
   int n;
@@ -97,8 +101,9 @@ struct RowsLoader {
     uint4 k[NK];
     uint32_t v[4][VPL / 2];
   };
-  MKV_DEV void start(int, Raw &) const {}
-  MKV_DEV void fetch(int tile, Raw &r) const {
+  MKV_DEV void start(int, Carry &) const {}
+  MKV_DEV void put_tables() const {}
+  MKV_DEV void fetch(int tile, Raw &r, Carry &) const {
     const int tid = threadIdx.x, last = n - 1;
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
@@ -146,97 +151,109 @@ struct RowsLoader {
 // Uniform 4-bit: a tile is one 64-token key block, the last one of an incomplete block fp16 rows.  A
 // value is (min + 8 step) + (code - 8) step, one fused operation a pair in fp16: taken from the middle of
 // the group's range, the step's rounding weighs as much as the value's own (from its minimum, codes of 7
-// or 8 times the step would carry 2.5 times that into values near 0).
+// or 8 times the step would carry 2.5 times that into values near 0).  A tile's middles and steps are read
+// and converted once, a thread per channel and per token group, one tile ahead of its codes, and put
+// into LDS in the order of the code pairs.
 template <int D>
 struct UqLoader {
   static constexpr bool kFix = false;
+  static constexpr int kDepth = 2;
   static constexpr int NK = D / 32, NGRP = D / 64, NW = D / 32;
   const uint8_t *kc, *vc;
   const float *kmeta, *vmeta;
   const uint16_t *kres;
+  int first_tile;
+  uint16_t *meta;  // LDS: two buffers of key middles, key steps [D] and value middles, value steps [NGRP][64]
   int n;
+  struct Carry {};
   struct Raw {
-    uint4 k[NK];     // codes of 8 channels in .x, or 8 fp16 keys
-    uint4 km[4];     // (min, step) of the thread's 8 channels
-    uint32_t v[NW];  // codes of D / 16 channels x 4 tokens
-    float2 vm[4][NGRP];
+    uint32_t k[NK], v[NW];
+    float mn, st;  // of the next tile: key channel tid, or value group (tid - D)
   };
-  MKV_DEV void start(int, Raw &) const {}
-  MKV_DEV void fetch(int tile, Raw &r) const {
-    const int tid = threadIdx.x, w = tid % (D / 8);
-    const bool whole = (tile + 1) * kTile <= n;
-#pragma unroll
-    for (int i = 0; i < NK; ++i) {
-      const int t = tid / (D / 8) + i * (2048 / D);
-      if (whole) r.k[i].x = gld(reinterpret_cast<const uint32_t *>(kc + (int64_t)(tile * kTile + t) * (D / 2)) + w);
-      else r.k[i] = gld16(kres + t * D + 8 * w);
+  MKV_DEV void fetch_meta(int tile, float &mn, float &st) const {
+    const int tid = threadIdx.x;
+    mn = st = 0.f;
+    const float *p = nullptr;
+    if (tid < D) {
+      if ((tile + 1) * kTile <= n) p = kmeta + ((int64_t)tile * D + tid) * 2;
+    } else if (tid < 2 * D && tile * kTile + (tid - D) / NGRP < n) {
+      p = vmeta + ((int64_t)tile * kTile * NGRP + tid - D) * 2;
     }
-    if (whole) {
+    if (p) {
+      const f2v x = gld(reinterpret_cast<const f2v *>(p));
+      mn = x[0];
+      st = x[1];
+    }
+  }
+  MKV_DEV void put_meta(int tile, float mn, float st) const {
+    const int tid = threadIdx.x;
+    if (tid >= 2 * D) return;
+    uint16_t *buf = meta + (tile & 1) * 4 * D;
+    int at;
+    if (tid < D) {
+      at = (tid & ~7) + 2 * (tid & 3) + ((tid >> 2) & 1);  // channels (0, 4), (1, 5), (2, 6), (3, 7) of 8
+    } else {
+      const int e = tid - D;
+      at = 2 * D + (e % NGRP) * kTile + e / NGRP;
+    }
+    buf[at] = f2h_bits(mn + 8.f * st);
+    buf[at + D] = f2h_bits(st);
+  }
+  float mn0, st0;  // the first tile's, until they are in LDS
+  MKV_DEV void start(int tile, Carry &) {
+    first_tile = tile;
+    fetch_meta(tile, mn0, st0);
+  }
+  MKV_DEV void put_tables() const { put_meta(first_tile, mn0, st0); }
+  MKV_DEV void fetch(int tile, Raw &r, Carry &) const {
+    const int tid = threadIdx.x, w = tid % (D / 8);
+    if ((tile + 1) * kTile <= n) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) r.km[i] = gld16(kmeta + ((int64_t)tile * D + 8 * w + 2 * i) * 2);
+      for (int i = 0; i < NK; ++i) {
+        const int t = tid / (D / 8) + i * (2048 / D);
+        r.k[i] = gld(reinterpret_cast<const uint32_t *>(kc + (int64_t)(tile * kTile + t) * (D / 2)) + w);
+      }
     }
     const int t0 = min(tile * kTile + 4 * (tid >> 4), (n - 1) & ~3);  // (slots come in fours)
     const uint32_t *vp = reinterpret_cast<const uint32_t *>(vc + (int64_t)t0 * (D / 2) + (tid & 15) * (D / 8));
 #pragma unroll
     for (int i = 0; i < NW; ++i) r.v[i] = gld(vp + i);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int g = 0; g < NGRP; ++g) {
-        const float *p = vmeta + ((int64_t)(t0 + j) * NGRP + g) * 2;
-        r.vm[j][g] = make_float2(gld(p), gld(p + 1));
-      }
+    fetch_meta(tile + 1, r.mn, r.st);
   }
   MKV_DEV void put(int tile, const Raw &r, Tile<D> &t) const {
     const int tid = threadIdx.x, w = tid % (D / 8);
+    const uint16_t *buf = meta + (tile & 1) * 4 * D;
     if ((tile + 1) * kTile <= n) {
-      uint32_t mid[4], st[4];  // channels (0, 4), (1, 5), (2, 6), (3, 7) of the thread's 8
-      float m[8], s[8];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        m[2 * i] = __builtin_bit_cast(float, r.km[i].x);
-        s[2 * i] = __builtin_bit_cast(float, r.km[i].y);
-        m[2 * i + 1] = __builtin_bit_cast(float, r.km[i].z);
-        s[2 * i + 1] = __builtin_bit_cast(float, r.km[i].w);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        mid[i] = pk_f16(m[i] + 8.f * s[i], m[i + 4] + 8.f * s[i + 4]);
-        st[i] = pk_f16(s[i], s[i + 4]);
-      }
+      const uint4 mid = *reinterpret_cast<const uint4 *>(buf + 8 * w), st = *reinterpret_cast<const uint4 *>(buf + D + 8 * w);
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
-        uint32_t x[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) x[c] = pk_fma(nib_pair(r.k[i].x, c), st[c], mid[c]);
-        const uint32_t o[4] = {pk_lo(x[0], x[1]), pk_lo(x[2], x[3]), pk_hi(x[0], x[1]), pk_hi(x[2], x[3])};
+        const uint32_t x0 = pk_fma(nib_pair(r.k[i], 0), st.x, mid.x), x1 = pk_fma(nib_pair(r.k[i], 1), st.y, mid.y);
+        const uint32_t x2 = pk_fma(nib_pair(r.k[i], 2), st.z, mid.z), x3 = pk_fma(nib_pair(r.k[i], 3), st.w, mid.w);
+        const uint32_t o[4] = {pk_lo(x0, x1), pk_lo(x2, x3), pk_hi(x0, x1), pk_hi(x2, x3)};
         put_k8(t, tid / (D / 8) + i * (2048 / D), 8 * w, o);
       }
-    } else {
+    } else {  // (the last tile of a sequence at most)
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
-        const uint32_t o[4] = {r.k[i].x, r.k[i].y, r.k[i].z, r.k[i].w};
-        put_k8(t, tid / (D / 8) + i * (2048 / D), 8 * w, o);
+        const int token = tid / (D / 8) + i * (2048 / D);
+        const uint4 u = gld16(kres + token * D + 8 * w);
+        const uint32_t o[4] = {u.x, u.y, u.z, u.w};
+        put_k8(t, token, 8 * w, o);
       }
     }
-    const int b = tid >> 4, rr = tid & 15, left = n - (tile * kTile + 4 * b);
+    const int b = tid >> 4, rr = tid & 15;
 #pragma unroll
     for (int g = 0; g < NGRP; ++g) {
-      float mid[4], st[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        mid[j] = j < left ? r.vm[j][g].x + 8.f * r.vm[j][g].y : 0.f;
-        st[j] = j < left ? r.vm[j][g].y : 0.f;
-      }
-      const uint32_t m01 = pk_f16(mid[0], mid[1]), m23 = pk_f16(mid[2], mid[3]);
-      const uint32_t s01 = pk_f16(st[0], st[1]), s23 = pk_f16(st[2], st[3]);
+      const uint2 mid = *reinterpret_cast<const uint2 *>(buf + 2 * D + g * kTile + 4 * b);
+      const uint2 st = *reinterpret_cast<const uint2 *>(buf + 3 * D + g * kTile + 4 * b);
 #pragma unroll
       for (int c = 0; c < 4; ++c) {  // channel 64 g + 4 rr + c: operand 4 g + c of the segment
         const uint32_t word = r.v[(4 * g + c) >> 1];
-        put_v(t, 64 * g + 4 * rr + c, b, pk_fma(nib_pair(word, 2 * (c & 1)), s01, m01),
-              pk_fma(nib_pair(word, 2 * (c & 1) + 1), s23, m23));
+        put_v(t, 64 * g + 4 * rr + c, b, pk_fma(nib_pair(word, 2 * (c & 1)), st.x, mid.x),
+              pk_fma(nib_pair(word, 2 * (c & 1) + 1), st.y, mid.y));
       }
     }
+    put_meta(tile + 1, r.mn, r.st);
   }
 };
 
@@ -245,12 +262,17 @@ struct UqLoader {
 template <int D, int BITS>
 struct KvqLoader {
   static constexpr bool kFix = true;
+  // (two tiles ahead it is no faster: 8 x 8192 tokens of 4 bits, 8 nodes, 52.8 us against 49.6.  Its
+  // table lookups keep the LDS busy half the time)
+  static constexpr int kDepth = 1;
   static constexpr int UK = kTile * D / 32, UV = kTile / 4 * D / 8;  // units of 32 keys, of 8 channels x 4 tokens
   const uint8_t *kc, *vc;
   const uint32_t *krow, *kout, *vout;
   const float *vsc;
-  const uint32_t *lutk, *lutv;  // LDS
-  const uint32_t *tau;          // LDS: thresholds of channel pairs
+  uint32_t *lutk, *lutv;  // LDS
+  uint32_t *tau;          // LDS: thresholds of channel pairs
+  uint4 lut4;             // this thread's part of the tables and thresholds until they are in LDS
+  uint32_t tau2;
   int n, cap, nov, rowbytes;
   bool outliers;
   // the tile's range of key outliers, and where its second 32 tokens begin; read one tile ahead of the
@@ -258,17 +280,32 @@ struct KvqLoader {
   struct Range {
     uint32_t e0, emid, e1;
   };
+  typedef Range Carry;
   struct Raw {
     uint32_t k[BITS], v[BITS];
     float s[4];
-    Range r, next;
+    Range r;
     uint32_t ko, vo;  // this thread's first key and value outlier
   };
   MKV_DEV Range range(int tile) const {
     return {gld(krow + min(tile * kTile, n)), gld(krow + min(tile * kTile + 32, n)), gld(krow + min(tile * kTile + 64, n))};
   }
-  MKV_DEV void start(int tile, Raw &r) const { r.next = range(tile); }
-  MKV_DEV void fetch(int tile, Raw &r) const {
+  MKV_DEV void start(int tile, Carry &next) const { next = range(tile); }
+  // The tables are read with the first tile and put into LDS behind its loads (all threads).
+  MKV_DEV void load_tables(const float *cbtab, const float *kmeta) {
+    static_assert(kTreeThreads * 4 >= 1024, "both tables of a codebook: one piece per thread");
+    const int tid = threadIdx.x;
+    lut4 = make_uint4(0u, 0u, 0u, 0u);
+    if (tid < lut_half_words(BITS) / 2)
+      lut4 = gld16(reinterpret_cast<const uint32_t *>(cbtab + kLutBase) + lut_offset(BITS) + 4 * tid);
+    tau2 = tid < D / 2 ? pk_f16(gld(kmeta + 4 * tid), gld(kmeta + 4 * tid + 2)) : 0u;
+  }
+  MKV_DEV void put_tables() const {
+    const int tid = threadIdx.x;
+    if (tid < lut_half_words(BITS) / 2) reinterpret_cast<uint4 *>(lutk)[tid] = lut4;
+    if (tid < D / 2) tau[tid] = tau2;
+  }
+  MKV_DEV void fetch(int tile, Raw &r, Carry &next) const {
     const int tid = threadIdx.x;
     if (UK == kTreeThreads || tid < UK) {
       const int t = min(tile * kTile + tid / (D / 32), n - 1);
@@ -288,10 +325,10 @@ struct KvqLoader {
       r.s[3] = __builtin_bit_cast(float, s.w);
     }
     if (!outliers) return;
-    r.r = r.next;
+    r.r = next;
     if (r.r.e0 + tid < r.r.e1) r.ko = gld(kout + r.r.e0 + tid);
     if (tid < kTile) r.vo = gld(vout + min(tile * kTile + tid, n - 1));
-    r.next = range(tile + 1);
+    next = range(tile + 1);
   }
   // bits [at, at + 2 BITS) of a unit, as the packed pair they stand for
   MKV_DEV uint32_t pair(const uint32_t *lut, const uint32_t (&w)[BITS], int f) const {
@@ -364,6 +401,7 @@ struct Rows {
   f4v o[G_::NM][RB];
   float m[RB], l[RB];
   unsigned long long mask[RB];  // the nodes that the row attends to
+  bool any;                     // some row exists (the same in all lanes)
 };
 
 // The wave's tokens of a tile in LDS: logits, softmax, output.  References and logits are kept unscaled; the
@@ -462,28 +500,37 @@ MKV_DEV void attend_tile(Tile<D> &t, Rows<D, RB, WR> &x, int left, float qscale)
   }
 }
 
-// A wave over tiles [begin, end) of the cache, each tile's loads issued before the one ahead of it is
-// computed; `first()` runs after the first loads are on their way.
+// Tiles [begin, end) of the cache, each tile's loads issued before the kDepth tiles ahead of it are computed; `first()` runs after the first loads are on their way.
 template <int D, int RB, int WR, class L, class F>
-MKV_DEV void attend_range(const L &ld, Tile<D> &t, Rows<D, RB, WR> &x, int begin, int end, float qscale, F first) {
-  typename L::Raw raw;
+MKV_DEV void attend_range(L &ld, Tile<D> &t, Rows<D, RB, WR> &x, int begin, int end, float qscale, F first) {
+  typename L::Raw raw[L::kDepth];
+  typename L::Carry carry;
   if (begin < end) {
-    ld.start(begin, raw);
-    ld.fetch(begin, raw);
+    ld.start(begin, carry);
+#pragma unroll
+    for (int i = 0; i < L::kDepth; ++i)
+      if (begin + i < end) ld.fetch(begin + i, raw[i], carry);
+    ld.put_tables();
   }
   first();
-  for (int tile = begin; tile < end; ++tile) {
-    ld.put(tile, raw, t);
-    __syncthreads();
-    if constexpr (L::kFix) {
-      if (ld.outliers) {  // (the same in all threads)
-        ld.fix(tile, raw, t);
-        __syncthreads();
+  __syncthreads();  // (the tables)
+  for (int tile = begin; tile < end;) {
+#pragma unroll
+    for (int i = 0; i < L::kDepth; ++i) {
+      if (tile >= end) break;  // (the same in all threads)
+      ld.put(tile, raw[i], t);
+      __syncthreads();
+      if constexpr (L::kFix) {
+        if (ld.outliers) {
+          ld.fix(tile, raw[i], t);
+          __syncthreads();
+        }
       }
+      if (tile + L::kDepth < end) ld.fetch(tile + L::kDepth, raw[i], carry);
+      if (x.any) attend_tile<D, RB, WR, false>(t, x, ld.n - tile * kTile, qscale);
+      __syncthreads();
+      ++tile;
     }
-    if (tile + 1 < end) ld.fetch(tile + 1, raw);
-    attend_tile<D, RB, WR, false>(t, x, ld.n - tile * kTile, qscale);
-    __syncthreads();
   }
 }
 
@@ -529,6 +576,7 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lq = lane >> 4;
   const int wr = wave / WT, wt = wave % WT;
   Rows<D, RB, WR> x;
+  x.any = yb * R + wr * RB * 16 < valid * G;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     const int row = yb * R + (wr * RB + rb) * 16 + lr, node = row / G;
@@ -553,7 +601,8 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
   nodes.stride = (int64_t)geo.Hkv * D;
   nodes.n = valid;
   typename RowsLoader<D>::Raw nraw;
-  if (tree) nodes.fetch(0, nraw);
+  typename RowsLoader<D>::Carry none;
+  if (tree) nodes.fetch(0, nraw, none);
   auto attend_nodes = [&]() {
     if (!tree) return;
     // A value that is infinite or NaN must reach only the rows that attend to its node: it is left out
@@ -570,7 +619,7 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
       }
     nodes.put(0, nraw, tile);
     const bool any_odd = __syncthreads_or(odd);
-    attend_tile<D, RB, WR, true>(tile, x, valid, qscale);
+    if (x.any) attend_tile<D, RB, WR, true>(tile, x, valid, qscale);
     if (any_odd && wt == 0) {
       for (int j = 0; j < valid; ++j)
 #pragma unroll
@@ -600,16 +649,12 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
     ld.kmeta = reinterpret_cast<const float *>(sd.kmeta) + h * stride_uq_kmeta(sd, D) * 2;
     ld.vmeta = reinterpret_cast<const float *>(sd.vmeta) + h * stride_uq_vmeta(sd, D) * 2;
     ld.kres = reinterpret_cast<const uint16_t *>(sd.kres) + (int64_t)h * kTile * D;
+    ld.meta = reinterpret_cast<uint16_t *>(s_lut);
     ld.n = n;
     attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale, attend_nodes);
   } else {
     auto run = [&](auto bits_tag) {
       constexpr int BITS = decltype(bits_tag)::value;
-      const uint32_t *lut = reinterpret_cast<const uint32_t *>(cbtab + kLutBase) + lut_offset(BITS);
-      for (int i = threadIdx.x; i < 2 * lut_half_words(BITS); i += kTreeThreads) s_lut[i] = gld(lut + i);
-      const float *tau = reinterpret_cast<const float *>(sd.kmeta) + (int64_t)h * D * 2;
-      if (threadIdx.x < D / 2) s_tau[threadIdx.x] = pk_f16(gld(tau + 4 * threadIdx.x), gld(tau + 4 * threadIdx.x + 2));
-      __syncthreads();
       KvqLoader<D, BITS> ld;
       ld.kc = reinterpret_cast<const uint8_t *>(sd.kc) + h * stride_codes(sd);
       ld.vc = reinterpret_cast<const uint8_t *>(sd.vc) + h * stride_codes(sd);
@@ -625,6 +670,7 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
       ld.nov = sd.nov_slots;
       ld.rowbytes = sd.rowbytes;
       ld.outliers = sd.bp > 0;
+      ld.load_tables(cbtab, reinterpret_cast<const float *>(sd.kmeta) + (int64_t)h * D * 2);
       attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale, attend_nodes);
     };
     if (sd.bits == 4) run(std::integral_constant<int, 4>{});
