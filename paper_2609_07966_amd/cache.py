@@ -127,9 +127,18 @@ class KVCache:
             else:
                 with torch.cuda.stream(self.stream):
                     out, ws = self._tree_buffers(q, n, out, ws)
-        L.mkv_tree_attention(self.h, _ptr(q), _ptr(k), _ptr(v), _ptr(mask), _ptr(n_valid), n, _ptr(out), _ptr(ws),
-                             ws.numel(), self.s)
+        self._launch(L.mkv_tree_attention, _ptr(q), _ptr(k), _ptr(v), _ptr(mask), _ptr(n_valid), n, _ptr(out), _ptr(ws),
+                     ws.numel())
         return out
+
+    def _launch(self, fn, *args):
+        """fn(handle, *args, stream) with the cache's device current."""
+        device = self.arena.device
+        if self.torch.cuda.current_device() == device.index:
+            fn(self.h, *args, self.s)
+        else:
+            with self.torch.cuda.device(device):
+                fn(self.h, *args, self.s)
 
     def _tree_buffers(self, q, n, out, ws):
         return self.torch.empty_like(q) if out is None else out, self.tree_workspace(n) if ws is None else ws
@@ -146,13 +155,13 @@ class KVCache:
         check_tensor("n_path", n_path, dev, torch.int32, (self.S,))
         if counts is not None:
             check_tensor("counts", counts, dev, torch.int32, (self.S,))
-        L.mkv_tree_accept(self.h, _ptr(k), _ptr(v), n, _ptr(path), _ptr(n_path), m, _ptr(counts), self.s)
+        self._launch(L.mkv_tree_accept, _ptr(k), _ptr(v), n, _ptr(path), _ptr(n_path), m, _ptr(counts))
 
     # ---- beams (mkv_cache_reorder) -------------------------------------------------------------
     def reorder(self, parent, width):
         """Beam w of group g takes the state of beam parent[g * width + w] (int32 [S]) of its group."""
         check_tensor("parent", parent, self.arena.device, self.torch.int32, (self.S,))
-        L.mkv_cache_reorder(self.h, _ptr(parent), width, self.s)
+        self._launch(L.mkv_cache_reorder, _ptr(parent), width)
 
     # ---- inspection --------------------------------------------------------------------------
     def export(self, seq, kv_head, what, dtype=None):

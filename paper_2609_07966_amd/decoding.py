@@ -36,27 +36,40 @@ def rope(xs, pos, inv_freq, sections=None, layout="halves", inverse=False, out=N
         raise ValueError(f"at most {L.ROPE_MAX_AXES} axes (got {len(sections)})")
     if layout not in L.ROPE_LAYOUTS:
         raise ValueError(f"layout must be one of {sorted(L.ROPE_LAYOUTS)} (got {layout!r})")
-    if out is None:
-        out = [x.new_empty(x.shape) for x in xs]
-    if len(out) != len(xs):
+    if out is not None and len(out) != len(xs):
         raise ValueError("out has another number of tensors than xs")
-    sets = []
-    for x, y in zip(xs, out):
-        shape, at = x.shape, []
-        if len(shape) != 3 or shape[0] != n_rows or shape[2] != d or y.shape != shape:
-            raise ValueError("xs and out are [rows][heads][head_dim] and agree in rows and head_dim, each pair in heads")
-        width = shape[1] * d
-        for t in (x, y):
-            if t.device != dev or t.dtype != torch.float16:
-                raise ValueError(f"xs and out must be float16 on {dev}")
-            stride = t.stride()
-            if stride[2] != 1 or (shape[1] > 1 and stride[1] != d):
-                raise ValueError("a row's heads must be contiguous (rows may be any distance apart)")
-            at.append(stride[0] if n_rows > 1 else width)  # (one row has any stride)
-        sets.append((x.data_ptr(), y.data_ptr(), at[0], at[1], shape[1]))
+    ys, sets = [], []
+    for i, x in enumerate(xs):
+        shape = x.shape
+        if len(shape) != 3 or shape[0] != n_rows or shape[2] != d:
+            raise ValueError("xs are [rows][heads][head_dim] and agree in rows and head_dim")
+        heads = shape[1]
+        x_stride = y_stride = heads * d
+        _rows(x, dev, heads, d)
+        if n_rows > 1:  # (one row has any stride)
+            x_stride = x.stride(0)
+        if out is None:
+            y = x.new_empty(shape)
+        else:
+            y = out[i]
+            if y.shape != shape:
+                raise ValueError("out has the shapes of xs")
+            _rows(y, dev, heads, d)
+            if n_rows > 1:
+                y_stride = y.stride(0)
+        ys.append(y)
+        sets.append((x.data_ptr(), y.data_ptr(), x_stride, y_stride, heads))
     if n_rows > 0:
         _launch(dev, L.mkv_rope, d, 2 * pairs, sections, layout, inv_freq.data_ptr(), pos.data_ptr(), n_rows, sets, inverse)
-    return out
+    return ys
+
+
+def _rows(t, dev, heads, d):
+    if t.device != dev or t.dtype != torch.float16:
+        raise ValueError(f"xs and out must be float16 on {dev}")
+    stride = t.stride()
+    if stride[2] != 1 or (heads > 1 and stride[1] != d):
+        raise ValueError("a row's heads must be contiguous (rows may be any distance apart)")
 
 
 def beam_workspace(n_batch, n_beams, vocab, n_select, device="cuda"):

@@ -174,6 +174,29 @@ def test_short_and_ragged(name):
     run_and_check(wl, 7, rng, valid=[7, 1, 0, 3, 7, -4, 9, 5])
 
 
+@pytest.mark.parametrize("bits,bp", [(4, 400), (3, 250), (2, 5000), (4, 0)])
+def test_outlier_budgets(bits, bp):
+    """Several value outliers a token, half of all values, and none: attention, acceptance, reordering."""
+    wl = workload(["KVQ4"] * 2, [130, 130], 4, 2, 128)
+    wl.cfg = lambda s: {"method": "kvq", "bits": bits, "outlier_bp": bp}
+    rng = np.random.default_rng(17)
+    run_and_check(wl, 6, rng)
+    a, _ = admitted(wl, 12, same=2)
+    b, _ = admitted(wl, 12, same=2)
+    _, kt, vt = drafts(wl, rng, 6)
+    path = np.tile(np.array([5, 0, 3, 1, 2], np.int32), (2, 1))
+    a.tree_accept(dev(kt), dev(vt), dev(path), dev(np.array([5, 0], np.int32)))
+    import torch
+    out = torch.empty((2, 4, 128), dtype=torch.float32, device="cuda")
+    for node in path[0]:
+        b.step(dev(kt[:, node]), dev(vt[:, node]), dev(drafts(wl, rng, 1)[0][:, 0]), out)
+    for h in range(2):
+        assert same_state(exports(a, 0, h, "kvq"), exports(b, 0, h, "kvq"))
+    a.reorder(dev(np.array([0, 0], np.int32)), 2)
+    for h in range(2):
+        assert same_state(exports(a, 1, h, "kvq"), exports(b, 0, h, "kvq"))
+
+
 def test_mixed_batch_and_splits():
     wl = workload(CONFIGS + ["FP16"], [3000, 1500, 900, 2047, 4100, 40], 8, 2, 128)
     run_and_check(wl, 12, np.random.default_rng(7))
