@@ -136,11 +136,12 @@ struct RowsLoader {
       put_k8(t, tid / (D / 8) + i * (2048 / D), 8 * (tid % (D / 8)), w);
     }
     const int b = tid >> 4, left = n - (tile * kTile + 4 * b);
+    const bool whole = (tile + 1) * kTile <= n;
 #pragma unroll
     for (int i = 0; i < VPL / 2; ++i) {
       uint32_t x[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = j < left ? r.v[j][i] : 0u;
+      for (int j = 0; j < 4; ++j) x[j] = whole || j < left ? r.v[j][i] : 0u;
       const int ch = VPL * (tid & 15) + 2 * i;
       put_v(t, ch, b, pk_lo(x[0], x[1]), pk_lo(x[2], x[3]));
       put_v(t, ch + 1, b, pk_hi(x[0], x[1]), pk_hi(x[2], x[3]));
@@ -404,7 +405,9 @@ struct Rows {
   bool any;                     // some row exists (the same in all lanes)
 };
 
-// The wave's tokens of a tile in LDS: logits, softmax, output.  References and logits are kept unscaled; the
+// The wave's tokens of a tile in LDS: all their logits, one move of the references, then the output 32 tokens
+// at a time, so that one step's exponentials can run under the products of the one before (2-6 % less than
+// logits 32 tokens at a time; two tiles in LDS with one barrier a tile gained nothing).  References and logits are kept unscaled; the
 // scale (and log2 e) enters with the reference in one fused operation before the exponential.
 // Tokens at or past `left` do not exist; MASKED: nor does, for a row, a token that its mask does not name.
 template <int D, int RB, int WR, bool MASKED>
@@ -413,58 +416,60 @@ MKV_DEV void attend_tile(Tile<D> &t, Rows<D, RB, WR> &x, int left, float qscale)
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lq = lane >> 4;
   const int tok0 = (wave % C::WT) * C::TW;
   const float lazy = kLazy / qscale;
-#pragma unroll 1
-  for (int u = 0; u < C::TW / (16 * C::NB); ++u) {
-    const int first = tok0 + 16 * C::NB * u;
-    f4v S[C::NB][RB];
+  constexpr int NT = C::TW / 16;  // 16-token blocks
+  f4v S[NT][RB];
 #pragma unroll
-    for (int b = 0; b < C::NB; ++b)
+  for (int b = 0; b < NT; ++b)
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) S[b][rb] = f4v{0.f, 0.f, 0.f, 0.f};
+    for (int rb = 0; rb < RB; ++rb) S[b][rb] = f4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int m = 0; m < C::NQ; ++m)
+  for (int b = 0; b < NT; ++b)
 #pragma unroll
-      for (int b = 0; b < C::NB; ++b) {
-        const h8v a = *reinterpret_cast<const h8v *>(t.k + (first + 16 * b + lr) * Tile<D>::KS + 32 * m + 8 * lq);
+    for (int m = 0; m < C::NQ; ++m) {
+      const h8v a = *reinterpret_cast<const h8v *>(t.k + (tok0 + 16 * b + lr) * Tile<D>::KS + 32 * m + 8 * lq);
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) S[b][rb] = mfma32(a, x.q[m][rb], S[b][rb]);
-      }
-    if (MASKED || first + 16 * C::NB > left) {
-#pragma unroll
-      for (int b = 0; b < C::NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int token = first + 16 * b + 4 * lq + i;
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb)
-            S[b][rb][i] = token < left && (!MASKED || ((x.mask[rb] >> token) & 1)) ? S[b][rb][i] : -INFINITY;
-        }
+      for (int rb = 0; rb < RB; ++rb) S[b][rb] = mfma32(a, x.q[m][rb], S[b][rb]);
     }
-    float mx[RB];
-    bool move = false;
+  if (MASKED || tok0 + C::TW > left) {
+#pragma unroll
+    for (int b = 0; b < NT; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int token = tok0 + 16 * b + 4 * lq + i;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+          S[b][rb][i] = token < left && (!MASKED || ((x.mask[rb] >> token) & 1)) ? S[b][rb][i] : -INFINITY;
+      }
+  }
+  float mx[RB];
+  bool move = false;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    mx[rb] = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < NT; ++b) {
+      mx[rb] = fmaxf(fmaxf(mx[rb], S[b][rb][0]), S[b][rb][1]);
+      mx[rb] = fmaxf(fmaxf(mx[rb], S[b][rb][2]), S[b][rb][3]);
+    }
+    move |= mx[rb] > x.m[rb] + lazy;
+  }
+  if (__any(move)) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      mx[rb] = -INFINITY;
+      float y = fmaxf(mx[rb], __shfl_xor(mx[rb], 16));
+      y = fmaxf(y, __shfl_xor(y, 32));
+      const bool up = y > x.m[rb];
+      const float corr = up ? fexp2((x.m[rb] - y) * qscale) : 1.f;
+      if (up) x.m[rb] = y;
+      x.l[rb] *= corr;
 #pragma unroll
-      for (int b = 0; b < C::NB; ++b) {
-        mx[rb] = fmaxf(fmaxf(mx[rb], S[b][rb][0]), S[b][rb][1]);
-        mx[rb] = fmaxf(fmaxf(mx[rb], S[b][rb][2]), S[b][rb][3]);
-      }
-      move |= mx[rb] > x.m[rb] + lazy;
+      for (int m = 0; m < C::NM; ++m) x.o[m][rb] *= corr;
     }
-    if (__any(move)) {
+  }
+  const char *vt = reinterpret_cast<const char *>(t.v);
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        float y = fmaxf(mx[rb], __shfl_xor(mx[rb], 16));
-        y = fmaxf(y, __shfl_xor(y, 32));
-        const bool up = y > x.m[rb];
-        const float corr = up ? fexp2((x.m[rb] - y) * qscale) : 1.f;
-        if (up) x.m[rb] = y;
-        x.l[rb] *= corr;
-#pragma unroll
-        for (int m = 0; m < C::NM; ++m) x.o[m][rb] *= corr;
-      }
-    }
+  for (int u = 0; u < NT / C::NB; ++u) {
+    const int first = tok0 + 16 * C::NB * u;
     uint32_t P[RB][2 * C::NB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
@@ -474,13 +479,12 @@ MKV_DEV void attend_tile(Tile<D> &t, Rows<D, RB, WR> &x, int left, float qscale)
       for (int b = 0; b < C::NB; ++b) {
         float p[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = fexp2(__builtin_fmaf(S[b][rb][i], qscale, ref));
+        for (int i = 0; i < 4; ++i) p[i] = fexp2(__builtin_fmaf(S[u * C::NB + b][rb][i], qscale, ref));
         x.l[rb] += (p[0] + p[1]) + (p[2] + p[3]);
         P[rb][2 * b] = pk_f16(p[0], p[1]);
         P[rb][2 * b + 1] = pk_f16(p[2], p[3]);
       }
     }
-    const char *vt = reinterpret_cast<const char *>(t.v);
     const uint32_t v0 = 2 * kTile * lr + 8 * ((first / 4 + lq) ^ vswz(lr));
 #pragma unroll
     for (int m = 0; m < C::NM; ++m) {
