@@ -17,22 +17,38 @@ TreePlan tree_plan(const Shape &sh, const std::vector<SeqDesc> &seqs, int n_node
   const int rows = n_nodes * sh.G;
   p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   p.row_blocks = (rows + p.rows - 1) / p.rows;
-  // all workgroups resident at once, by capacity: three a CU of the smaller ones, two of the larger
-  const int64_t target = (p.rows <= 32 ? 3 : 2) * kCus;
-  int longest = 0;
-  for (const SeqDesc &d : seqs) longest = std::max(longest, d.cap);
-  auto count = [&](int chunk) {
-    int64_t n = 0;
-    for (const SeqDesc &d : seqs) n += (d.cap + chunk - 1) / chunk;
-    return n * sh.Hkv * p.row_blocks;
-  };
-  int lo = 1, hi = std::max(1, (longest + kTreeTile - 1) / kTreeTile);  // tiles
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if (count(mid * kTreeTile) <= target) hi = mid;
-    else lo = mid + 1;
+  int longest = 0, quantized = 0;
+  int64_t tiles = 0;
+  for (const SeqDesc &d : seqs) {
+    longest = std::max(longest, d.cap);
+    quantized += d.method != FP16;
+    tiles += (d.cap + kTreeTile - 1) / kTreeTile + 1;
   }
-  p.chunk = lo * kTreeTile;
+  // the smallest split, by capacity, with at most `target` workgroups
+  auto chunk_for = [&](int64_t target) {
+    auto count = [&](int chunk) {
+      int64_t n = 0;
+      for (const SeqDesc &d : seqs) n += (d.cap + chunk - 1) / chunk;
+      return n * sh.Hkv * p.row_blocks;
+    };
+    int lo = 1, hi = std::max(1, (longest + kTreeTile - 1) / kTreeTile);  // tiles
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (count(mid * kTreeTile) <= target) hi = mid;
+      else lo = mid + 1;
+    }
+    return lo * kTreeTile;
+  };
+  // All workgroups are resident at once.  Where a CU has few tiles to go through, one workgroup each is
+  // best: every further split writes its rows' partial outputs, which the merge reads again, and without
+  // any split the merge's launch goes too (32 sequences of 300 fp16 tokens, 16 nodes: 19.2 us against 27.3
+  // with two a CU; 8 of 1024: 21.0 and 24.3; 2 of 4000: 21.4 and 24.5).  Over many tiles two (three of the
+  // smaller ones) hide each other's waits (8 of 8192 under KVQuant at 4 bits, 4 and 16 nodes: 45 and 65 us
+  // against 72 and 84; 8 of 4000 fp16 tokens: 35 against 39).  The limits lie where the two met.
+  p.chunk = chunk_for(kCus);
+  double few = quantized ? 6 : 12;
+  if (p.chunk >= longest && (!quantized || p.rows >= 64)) few *= 2;
+  if ((double)tiles * sh.Hkv * p.row_blocks > few * kCus) p.chunk = chunk_for((p.rows <= 32 ? 3 : 2) * kCus);
   p.max_splits = (longest + p.chunk - 1) / p.chunk;
   const SeqDesc &last = seqs.back();
   p.slots = (int)((last.row0 + (int64_t)(seqs.size() - 1) * (sh.max_new + 3)) / p.chunk + (int64_t)seqs.size() - 1 +
