@@ -5,9 +5,10 @@
 // vocabulary into registers and writes the chunk's best n_select logits, its maximum and its sum of
 // exponentials; a second, small launch has every request's candidates compared by their full scores
 // in float64 (two beams' scores lie closer than float32 tells apart once in some thousand selections).
-// Bound by reading the logits once.
+// Bound by reading the logits once (128 rows of 128000 float32: 65 MB in 18 us, 3.6 TB/s), small calls by the
+// two launches' latency (4 rows of 32001: 5 us each).
 //
-// Choosing the best K of a workgroup's values: the maxima over groups of 16 lanes are 64 values, and the
+// Choosing the best K of a workgroup's values: the maxima over its 64 groups of lanes are 64 values, and the
 // K-th largest of these (K <= 64) is not above the K-th largest of all.  Only the values that reach it are
 // collected (about K of random ones), as unique 64-bit keys (order-preserving bits of the value, then the
 // lower index first), and ranked against each other.  Where they do not fit the list (values in ascending
@@ -21,23 +22,25 @@ namespace mkv {
 
 namespace {
 
-constexpr int kBeamWaves = kBeamThreads / 64;
-constexpr int kBeamGroups = kBeamThreads / 16;
+constexpr int kScanWaves = kScanThreads / 64, kMergeThreads = 1024, kMergeWaves = kMergeThreads / 64;
+constexpr int kBeamGroups = 64;  // groups of lanes in either workgroup: of 8, of 16
 constexpr int kListCap = 2048;
-static_assert(2 * MKV_BEAM_MAX <= kBeamGroups && kBeamGroups == 64, "the K-th largest group maximum is taken by one wave");
+static_assert(2 * MKV_BEAM_MAX <= kBeamGroups && kScanThreads / 8 == kBeamGroups && kMergeThreads / 16 == kBeamGroups,
+              "the K-th largest group maximum is taken by one wave");
 
 typedef unsigned long long u64;
 
-// Largest value over each row of 16 lanes, in all its lanes.
+// Largest value over each group of N lanes (8 or 16), in all its lanes.
 template <int CTRL>
 MKV_DEV uint32_t dpp_u32(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false); }
-MKV_DEV uint32_t row_max_u32(uint32_t x) {
+template <int N>
+MKV_DEV uint32_t group_max(uint32_t x) {
   x = max(x, dpp_u32<0xB1>(x));
   x = max(x, dpp_u32<0x4E>(x));
   x = max(x, dpp_u32<0x141>(x));
-  return max(x, dpp_u32<0x140>(x));
+  return N == 16 ? max(x, dpp_u32<0x140>(x)) : x;
 }
-MKV_DEV u64 row_max_u64(u64 x) {
+MKV_DEV u64 group8_max(u64 x) {
   auto step = [&](auto ctrl) {
     constexpr int C = decltype(ctrl)::value;
     const u64 y = ((u64)dpp_u32<C>((uint32_t)(x >> 32)) << 32) | dpp_u32<C>((uint32_t)x);
@@ -46,7 +49,6 @@ MKV_DEV u64 row_max_u64(u64 x) {
   step(std::integral_constant<int, 0xB1>{});
   step(std::integral_constant<int, 0x4E>{});
   step(std::integral_constant<int, 0x141>{});
-  step(std::integral_constant<int, 0x140>{});
   return x;
 }
 
@@ -76,22 +78,22 @@ MKV_DEV u64 chunk_key(float x, int index) { return ((u64)float_key(x) << 32) | (
 
 // One workgroup per (chunk, row): E values a thread, in pieces of 4 contiguous ones.
 template <typename T, int E>
-__global__ __launch_bounds__(kBeamThreads) void k_beam_scan(const T *__restrict__ logits, int64_t row_stride, int vocab,
+__global__ __launch_bounds__(kScanThreads) void k_beam_scan(const T *__restrict__ logits, int64_t row_stride, int vocab,
                                                             int k, int n_chunks, BeamPartial *__restrict__ parts,
                                                             BeamCandidate *__restrict__ cands) {
   __shared__ PickLds L;
   __shared__ u64 s_list[kListCap];
-  __shared__ float s_max[kBeamWaves];
-  __shared__ double s_sum[kBeamWaves];
+  __shared__ float s_max[kScanWaves];
+  __shared__ double s_sum[kScanWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int chunk = blockIdx.x % n_chunks;
   const int64_t row = blockIdx.x / n_chunks;
   const T *p = logits + row * row_stride;
-  const int base = chunk * kBeamThreads * E;
+  const int base = chunk * kScanThreads * E;
   float x[E];
 #pragma unroll
   for (int i = 0; i < E / 4; ++i) {
-    const int at = base + (i * kBeamThreads + tid) * 4;
+    const int at = base + (i * kScanThreads + tid) * 4;
     float *f = x + 4 * i;
     if (at + 4 <= vocab) {
       if constexpr (sizeof(T) == 4) {
@@ -120,21 +122,21 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_scan(const T *__restrict_
     }
   }
   float mx = -INFINITY;
-  auto key_of = [&](int i, float v) { return chunk_key(v, base + ((i >> 2) * kBeamThreads + tid) * 4 + (i & 3)); };
+  auto key_of = [&](int i, float v) { return chunk_key(v, base + ((i >> 2) * kScanThreads + tid) * 4 + (i & 3)); };
 #pragma unroll
   for (int i = 0; i < E; ++i) {
     if (!(x[i] > -INFINITY)) x[i] = -INFINITY;  // NaN
     mx = fmaxf(mx, x[i]);
   }
-  const uint32_t gm = row_max_u32(float_key(mx));
-  if ((lane & 15) == 0) L.group[tid >> 4] = gm;
+  const uint32_t gm = group_max<8>(float_key(mx));
+  if ((lane & 7) == 0) L.group[tid >> 3] = gm;
   const float wm = wave_max(mx);
   if (lane == 0) s_max[wave] = wm;
   if (tid == 0) L.n = 0;
   __syncthreads();
   float M = s_max[0];
 #pragma unroll
-  for (int w = 1; w < kBeamWaves; ++w) M = fmaxf(M, s_max[w]);
+  for (int w = 1; w < kScanWaves; ++w) M = fmaxf(M, s_max[w]);
   if (wave == 0) {
     const uint32_t t = kth_of_64(L.group, k);
     if (lane == 0) L.tau = t;
@@ -163,7 +165,7 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_scan(const T *__restrict_
   const int n = L.n;
   BeamCandidate *out = cands + (row * n_chunks + chunk) * k;
   if (n <= kListCap) {
-    for (int i = tid; i < n; i += kBeamThreads) {
+    for (int i = tid; i < n; i += kScanThreads) {
       const u64 mine = s_list[i];
       int above = 0;
       for (int j = 0; j < n; ++j) above += s_list[j] > mine ? 1 : 0;
@@ -184,9 +186,9 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_scan(const T *__restrict_
         const u64 key = x[i] == -INFINITY ? 0 : key_of(i, x[i]);
         top = key < last && key > top ? key : top;
       }
-      const u64 g = row_max_u64(top);
+      const u64 g = group8_max(top);
       __syncthreads();
-      if ((lane & 15) == 0) L.group64[tid >> 4] = g;
+      if ((lane & 7) == 0) L.group64[tid >> 3] = g;
       __syncthreads();
       u64 all = 0;
       for (int i = 0; i < kBeamGroups; ++i) all = L.group64[i] > all ? L.group64[i] : all;
@@ -199,7 +201,7 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_scan(const T *__restrict_
   }
   if (tid == 0) {
     double total = 0.0;
-    for (int w = 0; w < kBeamWaves; ++w) total += s_sum[w];
+    for (int w = 0; w < kScanWaves; ++w) total += s_sum[w];
     parts[row * n_chunks + chunk] = {total, M, 0};
   }
 }
@@ -227,7 +229,7 @@ MKV_DEV Rank row_best(Rank x) {
 }
 
 // One workgroup per request.
-__global__ __launch_bounds__(kBeamThreads) void k_beam_merge(BeamArgs a, const BeamPartial *__restrict__ parts,
+__global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a, const BeamPartial *__restrict__ parts,
                                                              const BeamCandidate *__restrict__ cands, int n_chunks) {
   __shared__ double s_base[MKV_BEAM_MAX];  // scores[w] - lse(w); a finished beam: scores[w]
   __shared__ int s_done[MKV_BEAM_MAX];
@@ -236,13 +238,15 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_merge(BeamArgs a, const B
   __shared__ __attribute__((aligned(16))) uint32_t s_group32[kBeamGroups];
   __shared__ uint32_t s_tau;
   __shared__ int s_n;
-  constexpr int kCap = kListCap / 2;
+  constexpr int kCap = kListCap / 2, kAhead = 2;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int b = blockIdx.x, W = a.n_beams, K = a.n_select;
   const int per = n_chunks * K, total = W * per;
   auto cand_of = [&](int i) { return cands[(int64_t)b * total + i]; };
-  // (the thread's first candidate is on its way while the beams' sums are put together)
-  const BeamCandidate mine = cand_of(min(tid, total - 1));
+  // (the thread's first candidates are on their way while the beams' sums are put together)
+  BeamCandidate mine[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) mine[u] = cand_of(min(tid + u * kMergeThreads, total - 1));
   auto rank = [&](int i, const BeamCandidate &c) {
     const int w = i / per;
     if (s_done[w])
@@ -251,7 +255,7 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_merge(BeamArgs a, const B
     return Rank{double_key(s_base[w] + (double)c.logit), (u64)w * a.vocab + c.token};
   };
   if (tid == 0) s_n = 0;
-  for (int w = wave; w < W; w += kBeamWaves) {
+  for (int w = wave; w < W; w += kMergeWaves) {
     const int64_t row = (int64_t)b * W + w;
     float m = -INFINITY;
     for (int c = lane; c < n_chunks; c += 64) m = fmaxf(m, parts[row * n_chunks + c].max);
@@ -272,15 +276,19 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_merge(BeamArgs a, const B
   __syncthreads();
   // candidate i: beam i / per, the i % per-th of its chunks' candidates
   auto rank_of = [&](int i) { return rank(i, cand_of(i)); };
-  Rank best = {0, ~0ull};
-  if (tid < total) best = rank(tid, mine);
-  for (int i = tid + kBeamThreads; i < total; i += kBeamThreads) {
+  Rank best = {0, ~0ull}, ahead[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) {
+    const int i = tid + u * kMergeThreads;
+    ahead[u] = i < total ? rank(i, mine[u]) : Rank{0, ~0ull};
+    if (above(ahead[u], best)) best = ahead[u];
+  }
+  for (int i = tid + kAhead * kMergeThreads; i < total; i += kMergeThreads) {
     const Rank r = rank_of(i);
     if (above(r, best)) best = r;
   }
-  const Rank first = total <= kBeamThreads ? best : tid < total ? rank(tid, mine) : Rank{0, ~0ull};
   // the K-th best group by the upper half of its score
-  const uint32_t gm = row_max_u32((uint32_t)(best.score >> 32));
+  const uint32_t gm = group_max<16>((uint32_t)(best.score >> 32));
   if ((lane & 15) == 0) s_group32[tid >> 4] = gm;
   __syncthreads();
   if (wave == 0) {
@@ -294,9 +302,11 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_merge(BeamArgs a, const B
     const int at = atomicAdd(&s_n, 1);
     if (at < kCap) s_list[at] = r;
   };
-  collect(first);
-  if ((uint32_t)(best.score >> 32) >= tau)
-    for (int i = tid + kBeamThreads; i < total; i += kBeamThreads) collect(rank_of(i));
+  if ((uint32_t)(best.score >> 32) >= tau) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) collect(ahead[u]);
+    for (int i = tid + kAhead * kMergeThreads; i < total; i += kMergeThreads) collect(rank_of(i));
+  }
   __syncthreads();
   const int n = s_n;
   auto write = [&](int at, const Rank &r) {
@@ -306,7 +316,7 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_merge(BeamArgs a, const B
     a.score_out[o] = r.score ? (float)key_double(r.score) : -INFINITY;
   };
   if (n <= kCap) {
-    for (int i = tid; i < n; i += kBeamThreads) {
+    for (int i = tid; i < n; i += kMergeThreads) {
       const Rank mine = s_list[i];
       int before = 0;
       for (int j = 0; j < n; ++j) before += above(s_list[j], mine) ? 1 : 0;
@@ -317,7 +327,7 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_merge(BeamArgs a, const B
     Rank last = {~0ull, 0};
     for (int r = 0; r < K; ++r) {
       Rank top = {0, ~0ull};
-      for (int i = tid; i < total; i += kBeamThreads) {
+      for (int i = tid; i < total; i += kMergeThreads) {
         const Rank c = rank_of(i);
         if (above(last, c) && above(c, top)) top = c;
       }
@@ -340,11 +350,11 @@ hipError_t beam_impl(const BeamArgs &a, hipStream_t st) {
   BeamPartial *parts = static_cast<BeamPartial *>(a.workspace);
   BeamCandidate *cands = reinterpret_cast<BeamCandidate *>(parts + (int64_t)rows * chunks);
   auto kernel = beam_values(rows, a.vocab) == 16 ? k_beam_scan<T, 16> : k_beam_scan<T, 4>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)rows * chunks)), dim3(kBeamThreads), 0, st,
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)rows * chunks)), dim3(kScanThreads), 0, st,
                      static_cast<const T *>(a.logits), a.row_stride, a.vocab, a.n_select, chunks, parts, cands);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_beam_merge, dim3(a.n_batch), dim3(kBeamThreads), 0, st, a, parts, cands, chunks);
+  hipLaunchKernelGGL(k_beam_merge, dim3(a.n_batch), dim3(kMergeThreads), 0, st, a, parts, cands, chunks);
   return hipGetLastError();
 }
 

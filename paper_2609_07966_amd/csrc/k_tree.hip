@@ -14,9 +14,17 @@
 // their lanes.  One pass: running maximum and sum per row in float32; ranges are merged by their
 // maxima, waves through LDS and splits by a second launch.
 //
-// Roundings to fp16: dequantized keys and values (half a step, 2^-12 of the value on average; fp16 rows
-// and outliers exact), uniform steps before they multiply a code (2^-11 of it), and probabilities,
-// which are at most 2^kLazy at the running reference.  Everything summed is float32.
+// Roundings to fp16: dequantized keys and values (at most half a step, 2^-11 of the value; fp16 rows and
+// outliers are exact), uniform steps before they multiply a code (as much), and probabilities, which are at
+// most 2^kLazy at the running reference.  Everything summed is float32.  Against 64 bits the outputs of
+// quantized caches are 5e-4 off (2-norm), of fp16 ones 2.2e-4, of which their own rounding is 2.1e-4.  (Keys
+// in two fp16 parts would need half as many products again.)
+//
+// What bounds it (8 sequences of 8192 tokens, 32 query and 8 kv heads of 128): few rows, the cache's bytes
+// (fp16, 1 to 16 nodes: 5.3 to 4.7 TB/s; the quantized tiles cost more than their bytes, in table lookups and
+// conversion: uniform 4-bit 2.3 TB/s, KVQuant at 4 bits 1.8); many, the matrix units, the exponentials
+// and the LDS together (64 nodes: 550 to 610 TFLOP/s, where a large fp16 product of the library reaches 1320).
+
 #include <algorithm>
 
 #include "append_dev.h"
@@ -158,7 +166,7 @@ struct RowsLoader {
 template <int D>
 struct UqLoader {
   static constexpr bool kFix = false;
-  static constexpr int kDepth = 2;
+  static constexpr int kDepth = 2;  // (8 x 8192 tokens, 1 and 64 nodes: 43 and 142 us one tile ahead, 37 and 118 so)
   static constexpr int NK = D / 32, NGRP = D / 64, NW = D / 32;
   const uint8_t *kc, *vc;
   const float *kmeta, *vmeta;
@@ -844,8 +852,8 @@ hipError_t tree_rows(const Dev &dv, const Shape &sh, const TreePlan &plan, const
 // rounded float32 steps as the decode append (append_dev.h), whose codes it gives bit for bit.  What a token
 // needs of the ones before it: its place among the key outliers, from the waves' counts; the 4-token value
 // blocks, put together in LDS; the rows of a uniform 4-bit key block, which ends a group of tokens.
-// Bound by latency: two round trips and two barriers a group (8 tokens of KVQuant 4-bit one after another
-// by the append's workgroup of D threads take 33 us, so 5).
+// Bound by latency: two round trips and two barriers a group.  (One token after another by the append's
+// own workgroup: up to six of KVQuant at 3 bits for 256 heads 25 us, so 6.4; 64 tokens of 4 bits 243 and 27.)
 constexpr int kAcceptWaves = 8;
 
 template <int D>

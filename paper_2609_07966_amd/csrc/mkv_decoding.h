@@ -31,7 +31,7 @@ struct BeamArgs {
   int32_t n_batch, n_beams, vocab, n_select, pad_token;
   bool half;
 };
-constexpr int kBeamThreads = 1024;
+constexpr int kScanThreads = 512;
 struct BeamPartial {  // of a chunk of one beam's logits
   double sum;         // sum of 2^((x - max) log2 e)
   float max;
@@ -43,9 +43,9 @@ struct BeamCandidate {
 };
 // Logits per thread of a scan workgroup: 16 where that still leaves one for every CU, else 4.
 inline int beam_values(int n_rows, int vocab) {
-  return (int64_t)n_rows * ((vocab - 1) / (16 * kBeamThreads) + 1) >= kCus ? 16 : 4;
+  return (int64_t)n_rows * ((vocab - 1) / (16 * kScanThreads) + 1) >= kCus ? 16 : 4;
 }
-inline int beam_chunks(int n_rows, int vocab) { return (vocab - 1) / (kBeamThreads * beam_values(n_rows, vocab)) + 1; }
+inline int beam_chunks(int n_rows, int vocab) { return (vocab - 1) / (kScanThreads * beam_values(n_rows, vocab)) + 1; }
 inline size_t beam_workspace(int n_batch, int n_beams, int vocab, int n_select) {
   const int rows = n_batch * n_beams;
   return (size_t)rows * beam_chunks(rows, vocab) * (sizeof(BeamPartial) + n_select * sizeof(BeamCandidate));
