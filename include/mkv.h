@@ -377,6 +377,7 @@ mkv_status mkv_probe_read_bandwidth(const void *buf, size_t bytes, uint32_t *sin
  */
 #define MKV_ROPE_MAX_AXES 4
 #define MKV_ROPE_MAX_SETS 4
+#define MKV_ROPE_MAX_HEADS 8192
 typedef enum { MKV_ROPE_HALVES = 0, MKV_ROPE_PAIRS = 1 } mkv_rope_layout;
 
 typedef struct {
@@ -391,7 +392,7 @@ typedef struct {
   const uint16_t *x;
   uint16_t *y;
   int64_t x_stride, y_stride;  /* elements from one row to the next, >= n_heads * head_dim */
-  int32_t n_heads;             /* >= 1 */
+  int32_t n_heads;             /* 1..MKV_ROPE_MAX_HEADS */
 } mkv_rope_set;
 
 mkv_status mkv_rope(const mkv_rope_spec *spec, const float *inv_freq, const int32_t *pos, int32_t n_rows,
@@ -453,7 +454,8 @@ mkv_status mkv_tree_accept(mkv_cache *cache, const uint16_t *k, const uint16_t *
  * formed and compared in 64 bits (the exponentials under the logarithm in 32, their sum in 64); ties
  * go to the lower w * vocab + t.  A NaN logit counts as -infinity, and a continuation whose score is
  * not above -infinity (a dead beam's, a banned token's, or NaN) is never chosen: where fewer than
- * n_select are left, the last outputs are (parent 0, pad_token) with the score -infinity.
+ * n_select are left, the last outputs are (parent 0, pad_token) with the score -infinity.  (A +infinity
+ * logit makes every score of its beam NaN.)
  *   logits     device float32 (MKV_F32) or fp16 (MKV_F16) [n_batch * n_beams] rows of `vocab` values,
  *              row r at logits + r * row_stride (elements, >= vocab)
  *   scores     device float32 [n_batch][n_beams]

@@ -89,6 +89,13 @@ mkv_status check_tree(const mkv_cache *c, int n_nodes, const char *what) {
   return MKV_OK;
 }
 
+// A call's rows and splits, which the cache's layout settles: worked out once per number of nodes.
+const TreePlan &plan_of(mkv_cache *c, int n_nodes) {
+  TreePlan &p = c->tree_plans[n_nodes];
+  if (p.rows == 0) p = tree_plan(c->sh, c->hs, n_nodes);
+  return p;
+}
+
 mkv_status check_workspace(const void *p, size_t bytes, size_t need) {
   if (need == 0) return MKV_OK;
   if (!p) return fail(MKV_EINVAL, "workspace is NULL, %zu bytes are needed", need);
@@ -138,7 +145,8 @@ mkv_status mkv_rope(const mkv_rope_spec *spec, const float *inv_freq, const int3
   for (int i = 0; i < n_sets; ++i) {
     const mkv_rope_set &t = sets[i];
     if (!t.x || !t.y) return fail(MKV_EINVAL, "set %d: x and y must be non-NULL", i);
-    if (t.n_heads < 1 || t.n_heads > 65536) return fail(MKV_EINVAL, "set %d: n_heads must be 1..65536", i);
+    if (t.n_heads < 1 || t.n_heads > MKV_ROPE_MAX_HEADS)
+      return fail(MKV_EINVAL, "set %d: n_heads must be 1..%d", i, MKV_ROPE_MAX_HEADS);
     const int64_t row = (int64_t)t.n_heads * d;
     if (t.x_stride < row || t.y_stride < row) return fail(MKV_EINVAL, "set %d: a row stride is below n_heads * head_dim", i);
     if (t.x == t.y && t.x_stride != t.y_stride) return fail(MKV_EINVAL, "set %d: in place needs equal strides", i);
@@ -162,7 +170,7 @@ mkv_status mkv_tree_workspace(mkv_cache *c, int32_t n_nodes, size_t *bytes) {
   if (!bytes) return fail(MKV_EINVAL, "bytes is NULL");
   const mkv_status st = check_tree(c, n_nodes, "mkv_tree_workspace");
   if (st != MKV_OK) return st;
-  *bytes = tree_plan(c->sh, c->hs, n_nodes).bytes;
+  *bytes = plan_of(c, n_nodes).bytes;
   return MKV_OK;
 }
 
@@ -173,7 +181,7 @@ mkv_status mkv_tree_attention(mkv_cache *c, const uint16_t *q, const uint16_t *k
   if (st != MKV_OK) return st;
   if (!q || !k || !v || !mask || !out) return fail(MKV_EINVAL, "q, k, v, mask and out must be non-NULL");
   if ((st = check_idle(c, "mkv_tree_attention")) != MKV_OK) return st;
-  const TreePlan plan = tree_plan(c->sh, c->hs, n_nodes);
+  const TreePlan &plan = plan_of(c, n_nodes);
   if ((st = check_workspace(workspace, workspace_bytes, plan.bytes)) != MKV_OK) return st;
   const TreeArgs a{q, k, v, mask, n_valid, out, static_cast<float *>(workspace), n_nodes};
   return check_hip(launch_tree_attention(c->dv, c->sh, plan, a, static_cast<hipStream_t>(stream)), "tree attention");

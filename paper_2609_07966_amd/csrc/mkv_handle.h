@@ -3,7 +3,7 @@
 
 #include <vector>
 
-#include "mkv_internal.h"
+#include "mkv_decoding.h"
 
 namespace mkv {
 
@@ -25,6 +25,7 @@ struct mkv_cache {
   bool any_h2o = false, any_rocket = false, h2o_done = false, snap_done = false;
   int topk_max = 0;
   int h2o_rows = 0, rocket_rows = 0;
+  mkv::TreePlan tree_plans[MKV_TREE_MAX_NODES + 1] = {};  // by number of nodes; rows 0: not worked out yet
   // profiling
   bool evict_pending = false;  // H2O: the last eviction call's victims await the next decode append
   int prof_mask = 0;  // bit k: launches of kind k are timed

@@ -296,6 +296,7 @@ def test_accept_is_the_decode_append(d):
     kt *= 3
     path = np.stack([rng.permutation(n)[:m] for _ in names]).astype(np.int32)
     path[2, 6] = 12  # ends this path at six tokens
+    path[1, 3] = path[1, 2]  # a node twice
     counts = torch.zeros(len(names), dtype=torch.int32, device="cuda")
     a.tree_accept(dev(kt), dev(vt), dev(path), dev(np.array(took, np.int32)), counts)
     real = [9, 7, 6, 0, 5]
