@@ -15,8 +15,9 @@
 // maxima, waves through LDS and splits by a second launch.
 //
 // Roundings to fp16: dequantized keys and values (at most half a step, 2^-11 of the value; fp16 rows and
-// outliers are exact), uniform steps before they multiply a code (as much), and probabilities, which are at
-// most 2^kLazy at the running reference.  Everything summed is float32.  Against 64 bits the outputs of
+// outliers are exact), uniform steps before they multiply a code (as much), and probabilities, which are
+// formed 2^kLift times too large (2^15 at most, with the reference 2^kLazy behind), so that fp16 holds
+// them to half a step down to 2^-27 of the largest and a long tail of small ones is not lost.  Everything summed is float32.  Against 64 bits the outputs of
 // quantized caches are 5e-4 off (2-norm), of fp16 ones 2.2e-4, of which their own rounding is 2.1e-4.  (Keys
 // in two fp16 parts would need half as many products again.)
 //
@@ -36,7 +37,8 @@ namespace {
 
 constexpr int kTreeThreads = 256;
 constexpr int kTile = kTreeTile;
-constexpr float kLazy = 2.f;  // the reference of a row's softmax moves when a logit passes it by this (log2)
+constexpr float kLazy = 2.f;   // the reference of a row's softmax moves when a logit passes it by this (log2)
+constexpr float kLift = 13.f;  // probabilities are formed 2^kLift times too large: at most 2^15 in fp16
 
 typedef _Float16 h2v __attribute__((ext_vector_type(2)));
 typedef _Float16 h4v __attribute__((ext_vector_type(4)));
@@ -484,7 +486,7 @@ MKV_DEV void attend_tile(Tile<D> &t, Rows<D, RB, WR> &x, int left, float qscale)
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       // (a row that has seen nothing yet has no reference, and only logits of -infinity)
-      const float ref = x.m[rb] == -INFINITY ? 0.f : -x.m[rb] * qscale;
+      const float ref = x.m[rb] == -INFINITY ? 0.f : __builtin_fmaf(-x.m[rb], qscale, kLift);
 #pragma unroll
       for (int b = 0; b < C::NB; ++b) {
         float p[4];
@@ -697,7 +699,7 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
   for (int rb = 0; rb < RB; ++rb) {
     x.l[rb] += __shfl_xor(x.l[rb], 16);
     x.l[rb] += __shfl_xor(x.l[rb], 32);
-    x.m[rb] *= qscale;  // from here on in log2
+    x.m[rb] = __builtin_fmaf(x.m[rb], qscale, -kLift);  // from here on in log2, of what l and o are sums over
   }
   if constexpr (WT > 1) {
     // the waves that share rows: scaled to their common reference, then summed into the first

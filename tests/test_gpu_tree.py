@@ -268,6 +268,29 @@ def test_unaligned_tensors_and_large_logits():
     check(wl, held, 0, q[0], kt[0], vt[0], mask[0], got[0], 5)
 
 
+@pytest.mark.parametrize("n", [1, 16, 64])
+def test_many_small_weights(n):
+    """One token has nearly all the weight and a value of 0; the output is the tail's, 2^-25.5 each, which
+    the roundings above keep to u a value like any other."""
+    from types import SimpleNamespace
+
+    from paper_2609_07966_amd.cache import KVCache
+    t, hq, hkv, d = 8192, 8, 2, 128
+    c = KVCache((1, hq, hkv, d, 4), [{"method": "fp16"}], [t])
+    k, v = np.zeros((t, hkv, d), np.float16), np.ones((t, hkv, d), np.float16)
+    k[:, :, 0] = -25  # logits of 8 * -25 / sqrt(128)
+    k[5], v[5] = 0, 0
+    c.append_prompt(dev(k), dev(v))
+    q = np.zeros((1, n, hq, d), np.float16)
+    q[..., 0] = 8
+    kt, vt = np.zeros((2, 1, n, hkv, d), np.float16)
+    mask = np.zeros((1, n), np.uint64)
+    got = c.tree_attention(dev(q), dev(kt), dev(vt), dev(mask.view(np.int64))).cpu().numpy()
+    kk, vv = [k[:, h].astype(np.float64) for h in range(hkv)], [v[:, h].astype(np.float64) for h in range(hkv)]
+    held = SimpleNamespace(method="fp16", keys=kk, vals=vv, kmag=kk, vmag=vv)
+    check(SimpleNamespace(group=hq // hkv, head_dim=d, n_kv_heads=hkv), held, 0, q[0], kt[0], vt[0], mask[0], got[0], n)
+
+
 def exports(c, s, h, method):
     from paper_2609_07966_amd import _lib
     kinds = {"fp16": ["counts", "positions"], "uq": ["counts", "codes_k", "codes_v", "scales_k", "scales_v"],
