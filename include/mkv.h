@@ -373,7 +373,7 @@ mkv_status mkv_probe_read_bandwidth(const void *buf, size_t bytes, uint32_t *sin
  *             its keys): x device fp16, head j of row r at x + r * x_stride + j * head_dim (strides
  *             in elements), y likewise.  y may be x with the
  *             same stride (in place); otherwise no output may overlap an input or another output.
- * n_rows = 0 is accepted and enqueues nothing.  One launch; may be captured.
+ * n_rows = 0 is accepted and enqueues nothing.  One launch (one for each 2^23 workgroups); may be captured.
  */
 #define MKV_ROPE_MAX_AXES 4
 #define MKV_ROPE_MAX_SETS 4
@@ -415,7 +415,8 @@ mkv_status mkv_rope(const mkv_rope_spec *spec, const float *inv_freq, const int3
  *              nodes that do not exist are ignored; a word of 0 leaves the cached tokens)
  *   n_valid    optional device int32 [S]: sequence s has only its first n_valid[s] nodes (clamped to
  *              0..n_nodes); the others are not read and their rows of `out` stay as they were
- *   out        device fp16 [S][n_nodes][Hq][d]; sums and softmax in 32 bits, rounded once
+ *   out        device fp16 [S][n_nodes][Hq][d]; sums and softmax in 32 bits, rounded once; may not
+ *              overlap an input
  *   workspace  device, >= mkv_tree_workspace(cache, n_nodes) bytes, 256-byte aligned, used until the
  *              call's work is done: calls that may overlap need one each.  NULL if 0 bytes are needed.
  * n_nodes is 1..MKV_TREE_MAX_NODES.  After prefill or a completed decode step; changes no state of
@@ -463,8 +464,9 @@ mkv_status mkv_tree_accept(mkv_cache *cache, const uint16_t *k, const uint16_t *
  *   token, parent, score_out  device int32, int32, float32 [n_batch][n_select], best first; parent
  *              is the beam within its request, as mkv_cache_reorder takes it
  *   workspace  device, >= mkv_beam_workspace() bytes, 256-byte aligned (see mkv_tree_attention)
- * n_beams 1..MKV_BEAM_MAX, n_select 1..min(2 * MKV_BEAM_MAX, vocab), pad_token 0..vocab-1.  Two launches; may be
- * captured.  n_batch = 0 is accepted and enqueues nothing.
+ * n_beams 1..MKV_BEAM_MAX, n_select 1..min(2 * MKV_BEAM_MAX, vocab), pad_token 0..vocab-1.  No output may
+ * overlap an input.  n_batch below 2^22; n_batch * n_beams below 2^23 rows of up to 8192 logits, longer ones
+ * counting once for each 8192 (MKV_EINVAL beyond).  Two launches; may be captured.  n_batch = 0 is accepted and enqueues nothing.
  */
 #define MKV_BEAM_MAX 32
 typedef enum { MKV_F32 = 0, MKV_F16 = 1 } mkv_dtype;

@@ -26,6 +26,13 @@ def check_tensor(name, t, device, dtype, shape):
                          f"(got {t.dtype}, {tuple(t.shape)} on {t.device})")
 
 
+def check_workspace(t, device):
+    """(Its size and alignment are the library's to check.)"""
+    import torch
+    if t.device != device or t.dtype != torch.uint8 or not t.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {device} (got {t.dtype} on {t.device})")
+
+
 class KVCache:
     """One mixed-configuration KV cache (one attention layer's worth).
 
@@ -120,6 +127,8 @@ class KVCache:
         if out is not None:
             check_tensor("out", out, dev, torch.float16, (self.S, n, self.Hq, self.D))
         ws = workspace
+        if ws is not None:
+            check_workspace(ws, dev)
         if out is None or ws is None:
             # memory allocated here belongs to the cache's stream
             if raw_stream(dev) == self.s:

@@ -110,8 +110,10 @@ mkv_status check_beam_sizes(int n_batch, int n_beams, int vocab, int n_select) {
   if (vocab < 1 || vocab > (1 << 30)) return fail(MKV_EINVAL, "vocab must be 1..2^30");
   if (n_select < 1 || n_select > std::min(2 * MKV_BEAM_MAX, vocab))
     return fail(MKV_EINVAL, "n_select must be 1..min(%d, vocab)", 2 * MKV_BEAM_MAX);
-  if ((int64_t)n_batch * n_beams > INT32_MAX || (int64_t)n_batch * n_beams * beam_chunks(n_batch * n_beams, vocab) > INT32_MAX)
-    return fail(MKV_EINVAL, "too many rows");
+  // a launch takes under 2^32 threads: one workgroup per chunk of a row, one per request
+  const int64_t rows = (int64_t)n_batch * n_beams;
+  if (n_batch >= 1 << 22 || rows >= 1 << 23 || rows * beam_chunks((int)rows, vocab) >= 1 << 23)
+    return fail(MKV_EINVAL, "too many rows: n_batch must be below 2^22 and n_batch * n_beams * (chunks of a row) below 2^23");
   return MKV_OK;
 }
 

@@ -48,15 +48,18 @@ MKV_DEV void store(uint16_t *p, const float *f) {
   else gst(p, f2h_bits(f[0]));
 }
 
+constexpr int64_t kMaxBlocks = 1 << 23;  // of a launch: it takes under 2^32 threads along an axis
+
 // A row's work is NC = pairs / VEC places (and, where values behind rotary_dim have to be copied, those
 // places too) times `slots` head slots; slot i takes heads i, i + slots, ...  A block holds whole rows,
 // or a part of one.
 template <int VEC, bool PAIRS>
-__global__ __launch_bounds__(kRopeThreads) void k_rope(RopeArgs a, int places, int slots, int rows_per_block) {
+__global__ __launch_bounds__(kRopeThreads) void k_rope(RopeArgs a, int places, int slots, int rows_per_block,
+                                                       int64_t first_row) {
   const int units = places * slots;
   const int local = blockIdx.y * kRopeThreads + threadIdx.x;
   const int r = local / units, u = local % units;
-  const int64_t row = (int64_t)blockIdx.x * rows_per_block + r;
+  const int64_t row = first_row + (int64_t)blockIdx.x * rows_per_block + r;
   if (r >= rows_per_block || row >= a.n_rows) return;
   const int place = u % places, slot = u / places, half = a.rot / 2, nc = half / VEC;
   float c[VEC], s[VEC];
@@ -125,11 +128,15 @@ hipError_t rope_impl(const RopeArgs &a, bool copy_tail, hipStream_t st) {
   const int per = (int)std::min<int64_t>(8, std::max<int64_t>(1, all / kFull));
   const int slots = (a.n_heads + per - 1) / per, units = places * slots;
   const int rows_per_block = std::max(1, kRopeThreads / units);
-  const dim3 grid((unsigned)((a.n_rows + (int64_t)rows_per_block - 1) / rows_per_block),
-                  (unsigned)((units + kRopeThreads - 1) / kRopeThreads));
+  const int64_t blocks = (a.n_rows + (int64_t)rows_per_block - 1) / rows_per_block;
   auto kernel = a.pairs_layout ? k_rope<VEC, true> : k_rope<VEC, false>;
-  hipLaunchKernelGGL(kernel, grid, dim3(kRopeThreads), 0, st, a, places, slots, rows_per_block);
-  return hipGetLastError();
+  for (int64_t first = 0; first < blocks; first += kMaxBlocks) {
+    const dim3 grid((unsigned)std::min(kMaxBlocks, blocks - first), (unsigned)((units + kRopeThreads - 1) / kRopeThreads));
+    hipLaunchKernelGGL(kernel, grid, dim3(kRopeThreads), 0, st, a, places, slots, rows_per_block, first * rows_per_block);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace

@@ -6,7 +6,7 @@ current stream of the tensors' device.
 import torch
 
 from . import _lib as L
-from .cache import check_tensor, raw_stream
+from .cache import check_tensor, check_workspace, raw_stream
 
 
 def _launch(device, fn, *args):
@@ -34,6 +34,8 @@ def rope(xs, pos, inv_freq, sections=None, layout="halves", inverse=False, out=N
     check_tensor("inv_freq", inv_freq, dev, torch.float32, (pairs,))
     if len(sections) > L.ROPE_MAX_AXES:
         raise ValueError(f"at most {L.ROPE_MAX_AXES} axes (got {len(sections)})")
+    if n_rows >= 2 ** 31:
+        raise ValueError("too many rows")
     if layout not in L.ROPE_LAYOUTS:
         raise ValueError(f"layout must be one of {sorted(L.ROPE_LAYOUTS)} (got {layout!r})")
     if out is not None and len(out) != len(xs):
@@ -94,6 +96,10 @@ def beam_select(logits, scores, n_select, finished=None, pad_token=0, workspace=
     stride = logits.stride(1) if w > 1 else logits.stride(0) if b > 1 else v
     token = torch.empty((b, n_select), dtype=torch.int32, device=dev)
     parent, score = torch.empty_like(token), scores.new_empty((b, n_select))
+    if workspace is not None:
+        check_workspace(workspace, dev)
+    if b * w >= 2 ** 31:
+        raise ValueError("too many rows")
     ws = workspace if workspace is not None else beam_workspace(b, w, v, n_select, dev)
     _launch(dev, L.mkv_beam_select, logits.data_ptr(), L.F16 if logits.dtype == torch.float16 else L.F32, stride, b, w, v,
             scores.data_ptr(), 0 if finished is None else finished.data_ptr(), pad_token, n_select, token.data_ptr(),

@@ -106,6 +106,13 @@ static void check_beam() {
   CHECK(run(2, 4, 1000, 8, 0, 1000, 0, nullptr, need, nullptr) == MKV_EINVAL);
   CHECK(run(1 << 27, 32, 1000, 8) == MKV_EINVAL);  // more rows than an int counts
   CHECK(mkv_beam_workspace(2, 4, 1000, 8, nullptr) == MKV_EINVAL && launches == 1);
+  // no launch of 2^32 threads: requests, rows, chunks of rows
+  CHECK(mkv_beam_workspace((1 << 22) - 1, 1, 32, 8, &need) == MKV_OK);
+  CHECK(mkv_beam_workspace(1 << 22, 1, 32, 8, &need) == MKV_EINVAL);
+  CHECK(mkv_beam_workspace((1 << 18) - 1, 32, 8192, 8, &need) == MKV_OK);
+  CHECK(mkv_beam_workspace(1 << 18, 32, 8192, 8, &need) == MKV_EINVAL);
+  CHECK(mkv_beam_workspace((1 << 18) - 1, 32, 8193, 8, &need) == MKV_EINVAL);
+  CHECK(mkv_beam_workspace(INT32_MAX, 32, 32, 8, &need) == MKV_EINVAL);
 }
 
 static void check_cache_calls() {

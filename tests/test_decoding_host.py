@@ -43,3 +43,15 @@ def test_wrapper_refusals():
                 dict(logits=z.transpose(0, 1)[:, :2]), dict(finished=torch.zeros((2, 3)))):
         with pytest.raises(ValueError):
             decoding.beam_select(**{**dict(logits=z, scores=s, n_select=3), **bad})
+    # a workspace that is not bytes, or not all there, or elsewhere
+    ws = torch.zeros(1 << 16, dtype=torch.uint8)
+    for bad in (ws.float(), ws[::2], ws.to("meta")):
+        with pytest.raises(ValueError):
+            decoding.beam_select(z, s, 3, workspace=bad)
+    # more rows than the library counts
+    n = 2 ** 31
+    wide = torch.empty((n, 1, 2), dtype=torch.float16, device="meta")
+    with pytest.raises(ValueError):
+        decoding.rope([wide], torch.empty((1, n), dtype=torch.int32, device="meta"), torch.empty(1, device="meta"))
+    with pytest.raises(ValueError):
+        decoding.beam_select(torch.empty((n, 1, 1), device="meta"), torch.empty((n, 1), device="meta"), 1)

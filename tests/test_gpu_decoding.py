@@ -51,6 +51,37 @@ def freqs(n):
     return (10000.0 ** (-np.arange(n) / n)).astype(np.float32)
 
 
+def test_rope_many_rows_and_many_heads():
+    """More rows than one launch has workgroups for (one a row here), in place; more heads than one grid
+    row, with values behind rotary_dim."""
+    import torch
+    from paper_2609_07966_amd import decoding
+    n, d = (1 << 24) + 3, 1022
+    if torch.cuda.mem_get_info()[0] < 48 << 30:
+        pytest.skip("needs 36 GB of device memory")
+    freq = torch.rand(d // 2, device="cuda")
+    pos = torch.arange(n, dtype=torch.int32, device="cuda").view(1, n)
+    x = torch.empty((n, 1, d), dtype=torch.float16, device="cuda")
+    rows = torch.tensor([0, 1, (1 << 23) - 1, 1 << 23, (1 << 24) - 1, 1 << 24, n - 1], device="cuda")
+    x[rows] = torch.randn((len(rows), 1, d), device="cuda").half()
+    few = decoding.rope([x[rows]], pos[:, rows].contiguous(), freq)[0]
+    decoding.rope([x], pos, freq, out=[x])
+    assert torch.equal(x[rows], few)
+    del x
+    heads, d, half = 8192, 1024, 511
+    xs = [torch.randn((1, heads, d), device="cuda").half() for _ in range(4)]
+    p = torch.tensor([[12345]], dtype=torch.int32, device="cuda")
+    ys = decoding.rope(xs, p, freq)
+    t = (freq.double() * 12345).view(1, 1, half)
+    for x, y in zip(xs, ys):
+        a, b = x[..., :half].double(), x[..., half:2 * half].double()
+        ref = torch.cat([a * t.cos() - b * t.sin(), b * t.cos() + a * t.sin()], -1)
+        mag = (a ** 2 + b ** 2).sqrt().repeat(1, 1, 2)
+        # the result's rounding (2^-11), and sine and cosine to 2^-19
+        assert bool(((y[..., :2 * half].double() - ref).abs() <= 2.0 ** -11 * ref.abs() + 2.0 ** -18 * mag + 2.0 ** -25).all())
+        assert torch.equal(y[..., 2 * half:], x[..., 2 * half:])
+
+
 @pytest.mark.parametrize("layout", ["halves", "pairs"])
 @pytest.mark.parametrize("rows,heads,d,sections", [
     (1, (1,), 2, [1]), (5, (4, 4), 64, [32]), (33, (32, 8), 128, [16, 24, 24]), (700, (16, 2), 128, [32]),
