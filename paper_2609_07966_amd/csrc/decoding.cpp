@@ -24,13 +24,14 @@ TreePlan tree_plan(const Shape &sh, const std::vector<SeqDesc> &seqs, int n_node
     quantized += d.method != FP16;
     tiles += (d.cap + kTreeTile - 1) / kTreeTile + 1;
   }
+  auto splits_for = [&](int chunk) {
+    int64_t n = 0;
+    for (const SeqDesc &d : seqs) n += (d.cap + chunk - 1) / chunk;
+    return n;
+  };
   // the smallest split, by capacity, with at most `target` workgroups
   auto chunk_for = [&](int64_t target) {
-    auto count = [&](int chunk) {
-      int64_t n = 0;
-      for (const SeqDesc &d : seqs) n += (d.cap + chunk - 1) / chunk;
-      return n * sh.Hkv * p.row_blocks;
-    };
+    auto count = [&](int chunk) { return splits_for(chunk) * sh.Hkv * p.row_blocks; };
     int lo = 1, hi = std::max(1, (longest + kTreeTile - 1) / kTreeTile);  // tiles
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
@@ -50,6 +51,7 @@ TreePlan tree_plan(const Shape &sh, const std::vector<SeqDesc> &seqs, int n_node
   if (p.chunk >= longest && (!quantized || p.rows >= 64)) few *= 2;
   if ((double)tiles * sh.Hkv * p.row_blocks > few * kCus) p.chunk = chunk_for((p.rows <= 32 ? 3 : 2) * kCus);
   p.max_splits = (longest + p.chunk - 1) / p.chunk;
+  p.splits = (int)splits_for(p.chunk);
   const SeqDesc &last = seqs.back();
   p.slots = (int)((last.row0 + (int64_t)(seqs.size() - 1) * (sh.max_new + 3)) / p.chunk + (int64_t)seqs.size() - 1 +
                   (last.cap + p.chunk - 1) / p.chunk);

@@ -553,7 +553,7 @@ MKV_DEV void attend_range(L &ld, Tile<D> &t, Rows<D, RB, WR> &x, int begin, int 
 
 // What the kernel and the merge need to agree on.
 struct TreeGeo {
-  int Hkv, G, N, max_splits, chunk, max_new, items, row_blocks;
+  int Hkv, G, N, max_splits, chunk, max_new, items, row_blocks, S, even;  // even: all sequences have max_splits
 };
 // Splits of sequence s (a tile range each, by its capacity), and its first slot among all sequences'.
 MKV_DEV int splits_of(const SeqDesc &sd, const TreeGeo &g) { return (sd.cap + g.chunk - 1) / g.chunk; }
@@ -561,8 +561,36 @@ MKV_DEV int64_t first_split(const SeqDesc &sd, int s, const TreeGeo &g) {
   // capacities are at most n0 + max_new + 3, so this many splits lie before it
   return (sd.row0 + (int64_t)s * (g.max_new + 3)) / g.chunk + s;
 }
-// Tiles per split of a sequence that holds n tokens (its drafted tokens are the last tile).
-MKV_DEV int tiles_per_split(int n, int splits) { return ((n + kTile - 1) / kTile + 1 + splits - 1) / splits; }
+// A sequence's tiles, its drafted tokens being the last one, are dealt to its splits as evenly as they go.
+struct TileRange {
+  int begin, end;
+};
+MKV_DEV int tiles_of(int n) { return (n + kTile - 1) / kTile + 1; }
+MKV_DEV TileRange tile_range(int tiles, int splits, int split) {
+  const int q = tiles / splits, r = tiles % splits, begin = split * q + min(split, r);
+  return {begin, begin + q + (split < r ? 1 : 0)};
+}
+// Which (sequence, kv head, split) an item is: the splits of a head next to each other, the heads of a
+// sequence next.  Only splits that exist are launched: a workgroup that ends at once takes its place on the
+// card before one that has work, which then waits (8 sequences of 3293 to 5398 tokens, 24 nodes: 67 us with
+// one item per sequence, head and split of the longest).
+struct Item {
+  int s, h, split;
+};
+MKV_DEV Item item_of(int item, const SeqDesc *seqs, const TreeGeo &g) {
+  if (g.even) return {item / g.max_splits / g.Hkv, item / g.max_splits % g.Hkv, item % g.max_splits};
+  const int lane = threadIdx.x & 63;
+  for (int s0 = 0;; s0 += 64) {
+    const int mine = s0 + lane < g.S ? g.Hkv * ((gld(&seqs[s0 + lane].cap) + g.chunk - 1) / g.chunk) : 0;
+    const int upto = wave_incl_scan(mine), all = __builtin_amdgcn_readlane(upto, 63);
+    if (item < all) {
+      const int l = __builtin_ctzll(__ballot(item < upto)), heads = __builtin_amdgcn_readlane(mine, l);
+      const int splits = heads / g.Hkv, at = item - (__builtin_amdgcn_readlane(upto, l) - heads);
+      return {s0 + l, at / splits, at % splits};
+    }
+    item -= all;
+  }
+}
 
 template <int D, int RB, int WR>
 __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(const SeqDesc *__restrict__ seqs,
@@ -578,18 +606,19 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
   static_assert(WT == 1 || sizeof(float) * R * D <= sizeof(tile), "the waves' outputs are merged in the tile");
   const int item = blockIdx.x, yb = blockIdx.y;
   if (item >= geo.items) return;
-  const int split = item % geo.max_splits, sh = item / geo.max_splits, h = sh % geo.Hkv, s = sh / geo.Hkv;
+  const Item it = item_of(item, seqs, geo);
+  const int s = __builtin_amdgcn_readfirstlane(it.s), h = __builtin_amdgcn_readfirstlane(it.h);  // (in scalar registers)
+  const int split = __builtin_amdgcn_readfirstlane(it.split);
   const SeqDesc &sd = seqs[s];
-  const int splits = splits_of(sd, geo);
-  if (split >= splits) return;
   const int n = state[((int64_t)s * geo.Hkv + h) * ST_WORDS + ST_COUNT];
   const int N = geo.N, G = geo.G, Hq = geo.Hkv * G;
   const int valid = a.n_valid ? min(max(a.n_valid[s], 0), N) : N;
   if (yb * R >= valid * G) return;
-  const int per = tiles_per_split(n, splits), tiles = (n + kTile - 1) / kTile;
-  const int begin = split * per, end = min(begin + per, tiles);
-  if (begin > tiles) return;
-  const bool tree = begin + per > tiles;  // the drafted tokens are tile number `tiles`
+  const int tiles = tiles_of(n);
+  const TileRange mine = tile_range(tiles, splits_of(sd, geo), split);
+  if (mine.begin == mine.end) return;
+  const bool tree = mine.end == tiles;
+  const int begin = mine.begin, end = tree ? tiles - 1 : mine.end;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lq = lane >> 4;
   const int wr = wave / WT, wt = wave % WT;
   Rows<D, RB, WR> x;
@@ -786,8 +815,7 @@ __global__ __launch_bounds__(256) void k_tree_merge(const SeqDesc *__restrict__ 
   if (node >= valid) return;
   const SeqDesc &sd = seqs[s];
   const int n = state[((int64_t)s * geo.Hkv + h) * ST_WORDS + ST_COUNT];
-  const int splits = splits_of(sd, geo), per = tiles_per_split(n, splits);
-  const int used = ((n + kTile - 1) / kTile + 1 + per - 1) / per;
+  const int used = min(splits_of(sd, geo), tiles_of(n));
   const int64_t step = (int64_t)geo.Hkv * geo.row_blocks * R * (D + 2);
   const float *part = a.workspace + ((first_split(sd, s, geo) * geo.Hkv + h) * geo.row_blocks + row / R) * (int64_t)(R * (D + 2));
   const float *ml = part + R * D + (row % R) * 2, *o = part + (row % R) * D + c;
@@ -826,8 +854,9 @@ __global__ __launch_bounds__(256) void k_tree_merge(const SeqDesc *__restrict__ 
 
 template <int D, int RB, int WR>
 hipError_t tree_impl(const Dev &dv, const Shape &sh, const TreePlan &plan, const TreeArgs &a, hipStream_t st) {
-  const int items = sh.S * sh.Hkv * plan.max_splits;
-  const TreeGeo geo{sh.Hkv, sh.G, a.n_nodes, plan.max_splits, plan.chunk, sh.max_new, items, plan.row_blocks};
+  const int items = plan.splits * sh.Hkv;
+  const TreeGeo geo{sh.Hkv,   sh.G,  a.n_nodes,       plan.max_splits, plan.chunk,
+                    sh.max_new, items, plan.row_blocks, sh.S,            plan.splits == sh.S * plan.max_splits};
   // the row blocks of a range are a multiple of 8 workgroups apart: on one XCD, whose L2 then holds the
   // range for all of them
   const dim3 grid((items + 7) & ~7, plan.row_blocks);

@@ -73,7 +73,8 @@ struct TreePlan {
   int row_blocks;  // per (sequence, kv head)
   int chunk;       // cached tokens per split, by capacity (a multiple of 64)
   int max_splits;  // of one sequence
-  int slots;       // splits of all sequences, at most
+  int splits;      // of all sequences
+  int slots;       // places for them in the workspace
   size_t bytes;    // workspace
 };
 TreePlan tree_plan(const Shape &sh, const std::vector<SeqDesc> &seqs, int n_nodes);

@@ -168,7 +168,7 @@ static void check_plan(const std::vector<int> &methods, const std::vector<int> &
   CHECK(p.chunk % kTreeTile == 0 && p.chunk > 0);
   CHECK(p.rows * p.row_blocks >= n * g && p.rows * (p.row_blocks - 1) < n * g);
   std::set<int64_t> used;
-  int most = 0;
+  int most = 0, all = 0;
   for (int s = 0; s < c.sh.S; ++s) {
     const SeqDesc &q = c.hs[s];
     const int splits = (q.cap + p.chunk - 1) / p.chunk;
@@ -181,10 +181,18 @@ static void check_plan(const std::vector<int> &methods, const std::vector<int> &
     // every tile and the drafted one in exactly one of the splits in use, however many tokens there are
     for (int m : {1, 63, 64, 65, q.cap / 2 + 1, q.cap}) {
       if (m < 1 || m > q.cap) continue;
-      const int tiles = (m + kTreeTile - 1) / kTreeTile, per = (tiles + 1 + splits - 1) / splits, in_use = (tiles + 1 + per - 1) / per;
-      CHECK(in_use <= splits && (in_use - 1) * per <= tiles && in_use * per > tiles);
+      const int tiles = (m + kTreeTile - 1) / kTreeTile + 1, in_use = std::min(splits, tiles), each = tiles / splits, more = tiles % splits;
+      int next = 0;
+      for (int i = 0; i < splits; ++i) {
+        const int begin = i * each + std::min(i, more), end = begin + each + (i < more);
+        CHECK(begin == next && (end > begin) == (i < in_use));
+        next = end;
+      }
+      CHECK(next == tiles);
     }
+    all += splits;
   }
+  CHECK(all == p.splits);
   CHECK(most == p.max_splits);
   CHECK(p.max_splits == 1 ? p.bytes == 0 : p.bytes == sizeof(float) * (size_t)p.slots * hkv * p.row_blocks * p.rows * (d + 2));
 }
