@@ -42,10 +42,11 @@ TreePlan tree_plan(const Shape &sh, const std::vector<SeqDesc> &seqs, int n_node
   };
   // All workgroups are resident at once.  Where a CU has few tiles to go through, one workgroup each is
   // best: every further split writes its rows' partial outputs, which the merge reads again, and without
-  // any split the merge's launch goes too (32 sequences of 300 fp16 tokens, 16 nodes: 19.2 us against 27.3
-  // with two a CU; 8 of 1024: 21.0 and 24.3; 2 of 4000: 21.4 and 24.5).  Over many tiles two (three of the
-  // smaller ones) hide each other's waits (8 of 8192 under KVQuant at 4 bits, 4 and 16 nodes: 45 and 65 us
-  // against 72 and 84; 8 of 4000 fp16 tokens: 35 against 39).  The limits lie where the two met.
+  // any split the merge's launch goes too (32 sequences of 300 fp16 tokens, 16 nodes: 19.5 us against 26.9
+  // with two a CU; 8 of 1024: 20.8 and 22.9; 2 of 4000: 20.8 and 23.4).  Over many tiles two (three of the
+  // smaller ones) hide each other's waits (8 of 8192 under KVQuant at 4 bits, 4 nodes: 71.9, 49.4 and 42.8 us
+  // with one, two and three, 16 nodes: 84.4, 59.8 and 76.8; 8 of 4000 fp16 tokens: 36.8, 34.5 and 42.4).
+  // More than fit at once are slower at every size measured.  The limits lie where the two met.
   p.chunk = chunk_for(kCus);
   double few = quantized ? 6 : 12;
   if (p.chunk >= longest && (!quantized || p.rows >= 64)) few *= 2;

@@ -142,18 +142,6 @@ MKV_DEV void for_regions(const SeqDesc &d, const Moves &mv, int h, int D, Visit 
   }
 }
 
-MKV_DEV void move_state(const Moves &mv, int32_t *state, int g, int h, int width, int Hkv) {
-  // the words of one column by one thread, as above
-  if (threadIdx.x >= ST_WORDS) return;
-  int32_t v[MKV_BEAM_MAX];
-#pragma unroll
-  for (int b = 0; b < MKV_BEAM_MAX; ++b)
-    if (b < width) v[b] = state[((int64_t)(g * width + mv.parent[b]) * Hkv + h) * ST_WORDS + threadIdx.x];
-#pragma unroll
-  for (int b = 0; b < MKV_BEAM_MAX; ++b)
-    if (b < width) state[((int64_t)(g * width + b) * Hkv + h) * ST_WORDS + threadIdx.x] = v[b];
-}
-
 template <int UNIT>
 struct UnitType {
   typedef u32x4 type;

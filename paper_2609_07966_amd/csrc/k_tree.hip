@@ -17,14 +17,17 @@
 // Roundings to fp16: dequantized keys and values (at most half a step, 2^-11 of the value; fp16 rows and
 // outliers are exact), uniform steps before they multiply a code (as much), and probabilities, which are
 // formed 2^kLift times too large (2^15 at most, with the reference 2^kLazy behind), so that fp16 holds
-// them to half a step down to 2^-27 of the largest and a long tail of small ones is not lost.  Everything summed is float32.  Against 64 bits the outputs of
-// quantized caches are 5e-4 off (2-norm), of fp16 ones 2.2e-4, of which their own rounding is 2.1e-4.  (Keys
-// in two fp16 parts would need half as many products again.)
+// them to half a step down to 2^-27 of the largest and a long tail of small ones is not lost.  Everything
+// summed is float32.  Against 64 bits the outputs of quantized caches are 4e-4 to 6.5e-4 off (2-norm), of
+// fp16 ones 2.2e-4, of which their own rounding is 2.1e-4.  (Most of it is the keys' rounding; keys in two
+// fp16 parts would need half as many products again, and a second key tile in the LDS.)
 //
 // What bounds it (8 sequences of 8192 tokens, 32 query and 8 kv heads of 128): few rows, the cache's bytes
-// (fp16, 1 to 16 nodes: 5.3 to 4.7 TB/s; the quantized tiles cost more than their bytes, in table lookups and
-// conversion: uniform 4-bit 2.3 TB/s, KVQuant at 4 bits 1.8); many, the matrix units, the exponentials
-// and the LDS together (64 nodes: 550 to 610 TFLOP/s, where a large fp16 product of the library reaches 1320).
+// (fp16, 1 to 16 nodes: 5.4 to 4.9 TB/s; the quantized tiles cost more than their bytes, in conversion and
+// table lookups: uniform 4-bit 2.4 TB/s, vector operations 60 % of the time; KVQuant at 4 bits 1.9, the LDS
+// half of the time); many, the matrix units, the exponentials and the LDS one after
+// another, two waves a SIMD being too few to overlap them (64 nodes: 590 to 650 TFLOP/s, where a large fp16
+// product of the library reaches 1320).
 
 #include <algorithm>
 
@@ -168,7 +171,9 @@ struct RowsLoader {
 template <int D>
 struct UqLoader {
   static constexpr bool kFix = false;
-  static constexpr int kDepth = 2;  // (8 x 8192 tokens, 1 and 64 nodes: 43 and 142 us one tile ahead, 37 and 118 so)
+  // (8 x 8192 tokens: within 3 % of one tile ahead at 1 to 64 nodes, either way.  The registers that it
+  // takes lead the compiler to KVQuant tiles that are 5 % faster at 128 rows, in the same kernel.)
+  static constexpr int kDepth = 2;
   static constexpr int NK = D / 32, NGRP = D / 64, NW = D / 32;
   const uint8_t *kc, *vc;
   const float *kmeta, *vmeta;
@@ -273,7 +278,7 @@ struct UqLoader {
 template <int D, int BITS>
 struct KvqLoader {
   static constexpr bool kFix = true;
-  // (two tiles ahead it is no faster: 8 x 8192 tokens of 4 bits, 8 nodes, 52.8 us against 49.6.  Its
+  // (two tiles ahead it is no faster: 8 x 8192 tokens of 4 bits, 8 nodes, 52.2 us against 49.6.  Its
   // table lookups keep the LDS busy half the time)
   static constexpr int kDepth = 1;
   static constexpr int UK = kTile * D / 32, UV = kTile / 4 * D / 8;  // units of 32 keys, of 8 channels x 4 tokens
@@ -417,8 +422,10 @@ struct Rows {
 
 // The wave's tokens of a tile in LDS: all their logits, one move of the references, then the output 32 tokens
 // at a time, so that one step's exponentials can run under the products of the one before (2-6 % less than
-// logits 32 tokens at a time; two tiles in LDS with one barrier a tile gained nothing).  References and logits are kept unscaled; the
-// scale (and log2 e) enters with the reference in one fused operation before the exponential.
+// logits 32 tokens at a time; two tiles in LDS with one barrier a tile gained nothing, and key rows without
+// bank conflicts instead of padded ones cost more address registers than they gained).  References and
+// logits are kept unscaled; the scale (and log2 e) enters with the reference in one fused operation before
+// the exponential.
 // Tokens at or past `left` do not exist; MASKED: nor does, for a row, a token that its mask does not name.
 template <int D, int RB, int WR, bool MASKED>
 MKV_DEV void attend_tile(Tile<D> &t, Rows<D, RB, WR> &x, int left, float qscale) {
@@ -517,7 +524,8 @@ MKV_DEV void attend_tile(Tile<D> &t, Rows<D, RB, WR> &x, int left, float qscale)
   __builtin_amdgcn_s_setprio(0);
 }
 
-// Tiles [begin, end) of the cache, each tile's loads issued before the kDepth tiles ahead of it are computed; `first()` runs after the first loads are on their way.
+// Tiles [begin, end) of the cache, each tile's loads issued before the kDepth tiles ahead of it are computed;
+// `first()` runs after the first loads are on their way.
 template <int D, int RB, int WR, class L, class F>
 MKV_DEV void attend_range(L &ld, Tile<D> &t, Rows<D, RB, WR> &x, int begin, int end, float qscale, F first) {
   typename L::Raw raw[L::kDepth];
