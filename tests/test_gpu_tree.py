@@ -291,6 +291,51 @@ def test_many_small_weights(n):
     check(SimpleNamespace(group=hq // hkv, head_dim=d, n_kv_heads=hkv), held, 0, q[0], kt[0], vt[0], mask[0], got[0], n)
 
 
+def test_kvquant_thresholds_and_queries_of_all_sizes():
+    """Channels whose prompt was 0 or tiny and whose accepted tokens are not (every value an outlier far past
+    its threshold), a channel at the end of fp16, and rows of queries that are far apart in size.  Queries are
+    small where keys are large, so that logits stay within some units."""
+    from gpu_harness import oracle_codebooks
+    wl = workload(["KVQ4", "KVQ3", "KVQ2"], [100, 100, 100], 4, 2, 64)
+    from paper_2609_07966_amd.cache import KVCache
+    cfgs = [wl.cfg(s) for s in range(3)]
+    books, flat = oracle_codebooks(wl)
+    from oracle.sequence import Sequence
+    rng = np.random.default_rng(19)
+    size = np.zeros(64)
+    size[8:16], size[16:24], size[24:40], size[40:48] = 2.0 ** -22, 2.0 ** -9, 1.0, 300.0
+    k = (rng.standard_normal((3, 100, 2, 64)) * size).astype(np.float16)
+    v = rng.standard_normal((3, 100, 2, 64)).astype(np.float16)
+    c = KVCache((3, 4, 2, 64, 8), cfgs, [100] * 3, codebooks=list(flat))
+    c.append_prompt(dev(k.reshape(300, 2, 64)), dev(v.reshape(300, 2, 64)))
+    n = 4
+    kt, vt = (rng.standard_normal((2, 3, n, 2, 64))).astype(np.float16)
+    kt[..., :4] *= 1000
+    kt[:, 0, :, 60] = 65504
+    path = np.tile(np.arange(n, dtype=np.int32), (3, 1))
+    c.tree_accept(dev(kt), dev(vt), dev(path), dev(np.full(3, n, np.int32)))
+    q = rng.standard_normal((3, n, 4, 64))
+    q[..., :4] *= 2.0 ** -9
+    q[..., 40:48] *= 2.0 ** -8
+    q[..., 60] = 2.0 ** -16
+    q[:, 0] *= 2.0 ** -6
+    q[:, 2] *= 2
+    q = q.astype(np.float16)
+    mask = np.zeros((3, n), np.uint64)
+    got = c.tree_attention(dev(q), dev(kt), dev(vt), dev(mask.view(np.int64))).cpu().numpy()
+    from types import SimpleNamespace
+    for s in range(3):
+        seq = Sequence(cfgs[s], k[s], v[s], 4, codebooks=books)
+        keys, vals = [], []
+        for h in range(2):
+            keys.append(np.vstack([seq.kq[h]["eff"], seq._kvq_k(kt[s, :, h], h)["eff"]]))
+            vals.append(np.vstack([seq.vq[h]["eff"], seq._kvq_v(vt[s, :, h])["eff"]]))
+        held = SimpleNamespace(method="kvq", keys=keys, vals=vals, kmag=[np.abs(x) for x in keys], vmag=[np.abs(x) for x in vals])
+        for i in (0, 1, 2, 3):
+            one = np.zeros(1, np.uint64)
+            check(wl, held, s, q[s, i:i + 1], kt[s, :1], vt[s, :1], one, got[s, i:i + 1], 1)
+
+
 def exports(c, s, h, method):
     from paper_2609_07966_amd import _lib
     kinds = {"fp16": ["counts", "positions"], "uq": ["counts", "codes_k", "codes_v", "scales_k", "scales_v"],
