@@ -588,7 +588,7 @@ struct Item {
 MKV_DEV Item item_of(int item, const SeqDesc *seqs, const TreeGeo &g) {
   if (g.even) return {item / g.max_splits / g.Hkv, item / g.max_splits % g.Hkv, item % g.max_splits};
   const int lane = threadIdx.x & 63;
-  for (int s0 = 0;; s0 += 64) {
+  for (int s0 = 0; s0 < g.S; s0 += 64) {
     const int mine = s0 + lane < g.S ? g.Hkv * ((gld(&seqs[s0 + lane].cap) + g.chunk - 1) / g.chunk) : 0;
     const int upto = wave_incl_scan(mine), all = __builtin_amdgcn_readlane(upto, 63);
     if (item < all) {
@@ -598,6 +598,7 @@ MKV_DEV Item item_of(int item, const SeqDesc *seqs, const TreeGeo &g) {
     }
     item -= all;
   }
+  return {0, 0, 0};  // (no item is past the last sequence)
 }
 
 template <int D, int RB, int WR>

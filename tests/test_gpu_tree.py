@@ -202,6 +202,15 @@ def test_mixed_batch_and_splits():
     run_and_check(wl, 12, np.random.default_rng(7))
 
 
+def test_many_ragged_sequences():
+    # more sequences than a wave has lanes, of which only some are split
+    lens = [40 + 3 * (s % 9) for s in range(70)]
+    for s, n in ((0, 900), (13, 2100), (63, 700), (64, 1500), (69, 1100)):
+        lens[s] = n
+    wl = workload([CONFIGS[s % 5] for s in range(70)], lens, 4, 2, 64)
+    run_and_check(wl, 3, np.random.default_rng(20))
+
+
 def test_masks():
     # empty words, words that name later nodes, nodes past the tree, and every node
     wl = workload(["FP16", "KVQ4", "UQ4-g64"], [100, 200, 300], 4, 2, 64)
