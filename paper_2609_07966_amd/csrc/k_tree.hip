@@ -18,7 +18,7 @@
 // outliers are exact), uniform steps before they multiply a code (as much), and probabilities, which are
 // formed 2^kLift times too large (2^15 at most, with the reference 2^kLazy behind), so that fp16 holds
 // them to half a step down to 2^-27 of the largest and a long tail of small ones is not lost.  Everything
-// summed is float32.  Against 64 bits the outputs of quantized caches are 4e-4 to 6.5e-4 off (2-norm), of
+// summed is float32.  Against 64 bits the outputs of quantized caches are 3e-4 to 1.1e-3 off (2-norm), of
 // fp16 ones 2.2e-4, of which their own rounding is 2.1e-4.  (Most of it is the keys' rounding; keys in two
 // fp16 parts would need half as many products again, and a second key tile in the LDS.)
 //
