@@ -756,9 +756,10 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
 #pragma unroll
       for (int w = 1; w < WT; ++w) M = fmaxf(M, s_m[w][row]);
       float Ls = 0.f;
+      // (without a maximum nothing was summed, or only NaN, which no maximum sees: it stays either way)
 #pragma unroll
-      for (int w = 0; w < WT; ++w) Ls += s_m[w][row] == -INFINITY ? 0.f : s_l[w][row] * fexp2(s_m[w][row] - M);
-      const float f = x.m[rb] == -INFINITY ? 1.f : fexp2(x.m[rb] - M);  // (nothing summed: zeros)
+      for (int w = 0; w < WT; ++w) Ls += s_m[w][row] == -INFINITY ? s_l[w][row] : s_l[w][row] * fexp2(s_m[w][row] - M);
+      const float f = x.m[rb] == -INFINITY ? 1.f : fexp2(x.m[rb] - M);
 #pragma unroll
       for (int m = 0; m < NM; ++m) x.o[m][rb] *= f;
       x.m[rb] = M;
@@ -849,8 +850,8 @@ __global__ __launch_bounds__(256) void k_tree_merge(const SeqDesc *__restrict__ 
 #pragma unroll
     for (int i = 0; i < kMergeLoads; ++i) {
       const float m = x[i][0];
-      if (p0 + i >= used || m == -INFINITY) continue;
-      const float w = fexp2(m - M);
+      if (p0 + i >= used) continue;
+      const float w = m == -INFINITY ? 1.f : fexp2(m - M);  // (no maximum: zeros, or NaN that is to be seen)
       Ls += x[i][1] * w;
       acc += v[i] * w;
     }
