@@ -54,6 +54,9 @@ MKV_DEV f4v mfma16(h4v a, h4v b, f4v c) { return __builtin_amdgcn_mfma_f32_16x16
 MKV_DEV uint32_t pk_lo(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 MKV_DEV uint32_t pk_hi(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 MKV_DEV uint32_t pk_f16(float lo, float hi) { return __builtin_bit_cast(uint32_t, h2v{(_Float16)lo, (_Float16)hi}); }
+MKV_DEV uint16_t f2h_toward_0(float x) {
+  return (uint16_t)__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, 0.f));
+}
 MKV_DEV uint32_t pk_mul(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2v, a) * __builtin_bit_cast(h2v, b));
 }
@@ -212,8 +215,12 @@ struct UqLoader {
       const int e = tid - D;
       at = 2 * D + (e % NGRP) * kTile + e / NGRP;
     }
-    buf[at] = f2h_bits(mn + 8.f * st);
-    buf[at + D] = f2h_bits(st);
+    // (where the range may end within a rounding of fp16's, middle and step are rounded towards 0: rounded
+    // up they can take a code's value past 65504, which is the greatest of the group then)
+    const float mid = __builtin_fmaf(8.f, st, mn);
+    const bool far = fabsf(mid) + 8.f * st > 65408.f;
+    buf[at] = far ? f2h_toward_0(mid) : f2h_bits(mid);
+    buf[at + D] = far ? f2h_toward_0(st) : f2h_bits(st);
   }
   float mn0, st0;  // the first tile's, until they are in LDS
   MKV_DEV void start(int tile, Carry &) {

@@ -3,7 +3,7 @@ at the end of fp16's range, full caches, and decode steps after an acceptance.""
 import numpy as np
 import pytest
 
-from test_gpu_tree import Held, admitted, check, dev, drafts, workload
+from test_gpu_tree import Held, U, admitted, check, dev, drafts, trees, workload
 
 pytestmark = pytest.mark.gpu
 
@@ -66,3 +66,92 @@ def test_a_nan_that_a_row_sees_is_shown(name, hq, hkv, d, n, lens):
     got = attend(c, bad, kt, vt, mask)
     assert np.all(np.isnan(got[:, 4]))
     rest_right(wl, books, q, kt, vt, mask, got, clean, [4])
+
+
+# ---- the end of fp16's range -----------------------------------------------------------------------------
+
+def bounded(keys, vals, ekey, evals, q, kt, vt, mask, out):
+    """One sequence: keys, vals [Hkv] of [n][d] and bounds e_k, e_v of their errors alike; q, out [N][Hq][d].
+
+    With u = 2^-11 (half an fp16 step relative to the value) an output is off by at most u |o| (its rounding)
+    + u sum p |v| (probabilities) + sum p e_v (values) + (exp(2 dl) - 1) sum p |v| (keys: a logit is off by at
+    most dl = sum |q| e_k / sqrt(d)) + 1e-5 sum p |v| (sums and exponentials in float32)."""
+    n, hq, d = q.shape
+    g = hq // len(keys)
+    for h in range(len(keys)):
+        for i in range(n):
+            seen = [j for j in range(n) if int(mask[i]) >> j & 1]
+            none = np.zeros((len(seen), d))
+            k, v = (np.vstack([x, y[seen, h].astype(np.float64)]) for x, y in ((keys[h], kt), (vals[h], vt)))
+            ek, ev = np.vstack([ekey[h], none]), np.vstack([evals[h], none])
+            qq = q[i, h * g:(h + 1) * g].astype(np.float64)
+            z = qq @ k.T / np.sqrt(d)
+            p = np.exp(z - z.max(1, keepdims=True))
+            p /= p.sum(1, keepdims=True)
+            ref, mag = p @ v, p @ np.abs(v)
+            dl = (np.abs(qq) @ ek.T).max(1, keepdims=True) / np.sqrt(d)
+            tol = U * np.abs(ref) + p @ ev + (U + np.expm1(2 * dl) + 1e-5) * mag
+            err = np.abs(out[i, h * g:(h + 1) * g].astype(np.float64) - ref)
+            assert np.all(err <= tol), (h, i, float(np.nanmax(err / tol)), bool(np.isfinite(out).all()))
+
+
+def uq_error(x, eff):
+    """x [...][64] groups, eff what their codes stand for: the value's own rounding, u |v|, and those of the
+    group's middle and step, a whole unit of each where the range ends at fp16's: 2 u (|mid| + |v - mid|)."""
+    mn, mx = (f(x.astype(np.float64), axis=-1, keepdims=True) for f in (np.min, np.max))
+    mid = mn + 8 * (mx - mn) / 15
+    return U * np.abs(eff) + 2 * U * (np.abs(mid) + np.abs(eff - mid)) + 2.0 ** -21
+
+
+def ranged(rng, shape, ends):
+    """Groups of 64 along the last axis, each between a pair of ends and touching both."""
+    x = np.empty(shape, np.float64)
+    pick = np.array(ends, np.float64)[rng.integers(0, len(ends), shape[:-1])]
+    x[:] = pick[..., :1] + (pick[..., 1:] - pick[..., :1]) * rng.random(shape)
+    x[..., 0], x[..., 63] = pick[..., 0], pick[..., 1]
+    return rng.permuted(x, axis=-1).astype(np.float16)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("what", ["values", "keys"])
+def test_uniform_groups_at_the_end_of_fp16(d, what):
+    """Groups whose least or greatest value is the last finite one, or near it."""
+    from oracle import uniform
+    from paper_2609_07966_amd.cache import KVCache
+    rng = np.random.default_rng(34)
+    lens, hq, hkv, n = [64, 150, 700], 4, 2, 6
+    t = sum(lens)
+    m = 65504.0
+    ends = [(0, m), (-m, m), (-m, 0), (m - 64, m), (-m, -60000), (m, m)] + [(float(x), m) for x in rng.integers(-m, m, 40)] + \
+        [(-m, float(x)) for x in rng.integers(-m, m, 40)] + [(float(x), 64064.0) for x in rng.integers(-m, 64000, 20)]
+    k, v = (rng.standard_normal((t, hkv, d)).astype(np.float16) for _ in range(2))
+    if what == "values":
+        v = ranged(rng, (t, hkv, d // 64, 64), ends).reshape(t, hkv, d)
+    else:  # channels 0 to 7 of every whole block
+        row = 0
+        for n0 in lens:
+            whole = n0 // 64 * 64
+            x = ranged(rng, (whole // 64, hkv, 8, 64), ends)  # [block][head][channel][token]
+            k[row:row + whole, :, :8] = x.transpose(0, 3, 1, 2).reshape(whole, hkv, 8)
+            row += n0
+    c = KVCache((3, hq, hkv, d, 4), [{"method": "uq", "bits": 4, "group": 64}] * 3, lens)
+    c.append_prompt(dev(k), dev(v))
+    q, kt, vt = (rng.standard_normal((3, n, h, d)).astype(np.float16) for h in (hq, hkv, hkv))
+    if what == "keys":  # logits of a few units, most of their terms from the large channels
+        q[..., :8] = (rng.standard_normal((3, n, hq, 8)) * 2.0 ** -13).astype(np.float16)
+    mask, _ = trees(rng, 3, n)
+    mask[:, 0] = 0
+    got = attend(c, q, kt, vt, mask)
+    row = 0
+    for s, n0 in enumerate(lens):
+        parts = [[], [], [], []]
+        for h in range(hkv):
+            kh, vh, whole = k[row:row + n0, h], v[row:row + n0, h], n0 // 64 * 64
+            ke, ve = uniform.effective_keys(kh, 4, 64), uniform.effective_values(vh, 4, 64)
+            ek, groups = np.zeros((n0, d)), lambda x: x.reshape(-1, 64, d).transpose(0, 2, 1)
+            ek[:whole] = uq_error(groups(kh[:whole]), groups(ke[:whole])).transpose(0, 2, 1).reshape(whole, d)
+            ev = uq_error(vh.reshape(n0, -1, 64), ve.reshape(n0, -1, 64)).reshape(n0, d)
+            for part, x in zip(parts, (ke, ve, ek, ev)):
+                part.append(x)
+        bounded(*parts, q[s], kt[s], vt[s], mask[s], got[s])
+        row += n0
