@@ -682,8 +682,8 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
     nodes.put(0, nraw, tile);
     const bool any_odd = __syncthreads_or(odd);
     if (x.any) attend_tile<D, RB, WR, true>(tile, x, valid, qscale);
-    if (any_odd && wt == 0) {
-      for (int j = 0; j < valid; ++j)
+    if (any_odd) {  // (by the waves that have the node's logit, and with it a maximum)
+      for (int j = wt * C::TW; j < min(valid, (wt + 1) * C::TW); ++j)
 #pragma unroll
         for (int m = 0; m < NM; ++m)
 #pragma unroll

@@ -155,3 +155,52 @@ def test_uniform_groups_at_the_end_of_fp16(d, what):
                 part.append(x)
         bounded(*parts, q[s], kt[s], vt[s], mask[s], got[s])
         row += n0
+
+
+@pytest.mark.parametrize("name", ["FP16", "UQ4-g64", "KVQ3"])
+@pytest.mark.parametrize("lens", [[63, 129], [900, 2100]])
+def test_rows_beside_a_node_that_is_not_finite(name, lens):
+    """Rows that attend to several nodes but not to the one whose key and value are not finite: against the
+    oracle with the whole of their masks."""
+    wl = workload([name] * 2, lens, 8, 2, 128)
+    rng = np.random.default_rng(33)
+    c, books = admitted(wl, 4)
+    n = 12
+    q, kt, vt = drafts(wl, rng, n)
+    mask, _ = trees(rng, 2, n)
+    mask &= ~np.uint64(1 << 3)
+    mask[:, 3] |= np.uint64(1 << 3)
+    mask[:, 11] |= np.uint64(0x7F7)
+    clean = attend(c, q, kt, vt, mask)
+    for bad in (np.nan, np.inf, -np.inf):
+        kb, vb = kt.copy(), vt.copy()
+        vb[:, 3] = bad
+        kb[:, 3, :, ::2] = bad
+        got = attend(c, q, kb, vb, mask)
+        assert not np.any(np.isfinite(got[:, 3]))
+        rest_right(wl, books, q, kt, vt, mask, got, clean, [3])
+
+
+@pytest.mark.parametrize("name", ["FP16", "KVQ3"])
+@pytest.mark.parametrize("hq,hkv,d,n", [(4, 4, 64, 13), (4, 4, 128, 40), (8, 4, 64, 24), (4, 4, 64, 64), (8, 2, 128, 50)])
+@pytest.mark.parametrize("lens", [[40], [70], [300] * 64, [1500]])
+def test_an_infinite_value_that_a_row_sees_stays_infinite(name, hq, hkv, d, n, lens):
+    """A node's infinite value has a positive weight in the rows that attend to it, whichever of the others
+    they see: the output is infinite there and what it was anywhere else."""
+    wl = workload([name] * len(lens), lens, hq, hkv, d)
+    rng = np.random.default_rng(32)
+    c, books = admitted(wl, 4)
+    q, kt, vt = drafts(wl, rng, n)
+    mask, _ = trees(rng, 1, n)
+    mask = np.tile(mask, (len(lens), 1))
+    mask[:, n - 1] = np.uint64(1 << (n - 1))  # a row that sees the last node alone
+    mask[:, n - 2] = np.uint64(3 << (n - 2))
+    clean = attend(c, q, kt, vt, mask)
+    for node, bad in ((n - 1, np.inf), (n - 2, -np.inf), (0, np.inf)):
+        odd = vt.copy()
+        odd[:, node, :, 5:9] = bad
+        got = attend(c, q, kt, odd, mask)
+        sees = [i for i in range(n) if int(mask[0, i]) >> node & 1]
+        assert np.all(got[:, sees][..., 5:9] == bad), node
+        if len(lens) == 1:
+            rest_right(wl, books, q, kt, vt, mask, got, clean, sees, slice(5, 9))
