@@ -566,6 +566,13 @@ MKV_DEV void attend_range(L &ld, Tile<D> &t, Rows<D, RB, WR> &x, int begin, int 
   }
 }
 
+// A weighted mean as fp16.  The weights' roundings can take it past the values it is a mean of by 2^-11: not
+// past the last finite one, which would round to infinity.
+MKV_DEV uint16_t mean_bits(float x) {
+  constexpr float kLast = 65504.f, kPast = kLast * (1.f + 2.f / 2048.f);
+  return f2h_bits(fabsf(x) < kPast ? fminf(fmaxf(x, -kLast), kLast) : x);
+}
+
 // What the kernel and the merge need to agree on.
 struct TreeGeo {
   int Hkv, G, N, max_splits, chunk, max_new, items, row_blocks, S, even;  // even: all sequences have max_splits
@@ -804,7 +811,7 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
 #pragma unroll
       for (int m = 0; m < NM; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) gst(op + 16 * m + 4 * lq + i, f2h_bits(x.o[m][rb][i] * inv));
+        for (int i = 0; i < 4; ++i) gst(op + 16 * m + 4 * lq + i, mean_bits(x.o[m][rb][i] * inv));
     }
     return;
   }
@@ -866,7 +873,7 @@ __global__ __launch_bounds__(256) void k_tree_merge(const SeqDesc *__restrict__ 
   uint16_t *op = a.out + (((int64_t)s * N + node) * Hq + h * G + row % G) * D + c;
   const float inv = 1.f / Ls;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) gst(op + i, f2h_bits(acc[i] * inv));
+  for (int i = 0; i < 4; ++i) gst(op + i, mean_bits(acc[i] * inv));
 }
 
 template <int D, int RB, int WR>

@@ -204,3 +204,44 @@ def test_an_infinite_value_that_a_row_sees_stays_infinite(name, hq, hkv, d, n, l
         assert np.all(got[:, sees][..., 5:9] == bad), node
         if len(lens) == 1:
             rest_right(wl, books, q, kt, vt, mask, got, clean, sees, slice(5, 9))
+
+
+@pytest.mark.parametrize("name", ["FP16", "UQ4-g64", "KVQ4"])
+@pytest.mark.parametrize("n0", [1, 5, 70, 700])
+def test_a_mean_of_last_finite_values_is_finite(name, n0):
+    """Every value of a channel is fp16's last finite one (or its negative): so is every weighted mean of
+    them, whichever way the weights were rounded."""
+    from paper_2609_07966_amd.cache import KVCache
+    rng = np.random.default_rng(35)
+    hq, hkv, d, n = 8, 2, 64, 64
+    wl = workload([name], [n0], hq, hkv, d)
+    books = np.concatenate([np.linspace(-1, 1, 1 << b) for b in (2, 3, 4) for _ in range(2)])
+    c = KVCache((1, hq, hkv, d, 4), [wl.cfg(0)], [n0], codebooks=[float(x) for x in books.astype(np.float16)])
+    k = (rng.standard_normal((n0, hkv, d)) * 2).astype(np.float16)
+    v = np.full((n0, hkv, d), 65504.0, np.float16)
+    v[:, :, ::3] = -65504.0
+    c.append_prompt(dev(k), dev(v))
+    q, kt, _ = drafts(wl, rng, n)
+    vt = np.broadcast_to(v[0], (1, n, hkv, d)).copy()
+    mask, _ = trees(rng, 1, n)
+    got = attend(c, q, kt, vt, mask).astype(np.float64)
+    want = np.broadcast_to(v[0, 0].astype(np.float64), got.shape)
+    # the weights' roundings (u), the values' (3 u, uniform 4-bit), the result's (u)
+    assert np.all(np.abs(got - want) <= 5 * U * 65504), np.abs(got).max()
+
+
+def test_one_weight_rounded_up_takes_no_value_past_the_end():
+    """A cached token whose weight is just over twice a node's, in steps of 2^-16 or so: where its fp16
+    probability is rounded up by half a step, the quotient lies above what it is a mean of."""
+    from paper_2609_07966_amd.cache import KVCache
+    n, hq, hkv, d = 64, 8, 2, 64
+    c = KVCache((1, hq, hkv, d, 4), [{"method": "fp16"}], [1])
+    k, v = np.zeros((1, hkv, d), np.float16), np.full((1, hkv, d), 65504.0, np.float16)
+    k[..., :2] = 1
+    c.append_prompt(dev(k), dev(v))
+    q, kt = np.zeros((1, n, hq, d), np.float16), np.zeros((1, n, hkv, d), np.float16)
+    q[..., 0] = 8 * np.log(2)  # the logit of the cached token is about log 2, that of the nodes 0
+    q[0, :, :, 1] = (np.arange(n * hq).reshape(n, hq) - 64) * 2.0 ** -14
+    mask = (np.uint64(1) << np.arange(n, dtype=np.uint64))[None]
+    got = attend(c, q, kt, np.full((1, n, hkv, d), 65504.0, np.float16), mask).astype(np.float64)
+    assert np.all(np.abs(got - 65504) <= 2 * U * 65504), got.max()
