@@ -57,6 +57,7 @@ MKV_DEV uint32_t pk_f16(float lo, float hi) { return __builtin_bit_cast(uint32_t
 MKV_DEV uint16_t f2h_toward_0(float x) {
   return (uint16_t)__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, 0.f));
 }
+constexpr uint32_t kOnePair = 0x3C003C00u;
 MKV_DEV uint32_t pk_mul(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2v, a) * __builtin_bit_cast(h2v, b));
 }
@@ -281,7 +282,9 @@ struct UqLoader {
 };
 
 // KVQuant: codes through tables of fp16 pairs (or, at 2 bits, quads), times the channel's threshold
-// (keys) or the token's scale (values), which are fp16 values themselves; then the outliers.
+// (keys) or the token's scale (values), which are fp16 values themselves; then the outliers.  A codebook may
+// go past 1, and its values past fp16's end: keys and values are then held times a power of two (cb_scale),
+// which goes into the tables and comes off the logits and outputs in float32.
 template <int D, int BITS>
 struct KvqLoader {
   static constexpr bool kFix = true;
@@ -294,6 +297,8 @@ struct KvqLoader {
   const float *vsc;
   uint32_t *lutk, *lutv;  // LDS
   uint32_t *tau;          // LDS: thresholds of channel pairs
+  float kscale, vscale;   // powers of two, at most 1
+  uint32_t scales;        // both as fp16, in a scalar register
   uint4 lut4;             // this thread's part of the tables and thresholds until they are in LDS
   uint32_t tau2;
   int n, cap, nov, rowbytes;
@@ -319,13 +324,21 @@ struct KvqLoader {
     static_assert(kTreeThreads * 4 >= 1024, "both tables of a codebook: one piece per thread");
     const int tid = threadIdx.x;
     lut4 = make_uint4(0u, 0u, 0u, 0u);
+    kscale = cbtab[cb_scale(BITS)];
+    vscale = cbtab[cb_scale(BITS) + 1];
+    scales = __builtin_amdgcn_readfirstlane(pk_f16(kscale, vscale));
     if (tid < lut_half_words(BITS) / 2)
       lut4 = gld16(reinterpret_cast<const uint32_t *>(cbtab + kLutBase) + lut_offset(BITS) + 4 * tid);
     tau2 = tid < D / 2 ? pk_f16(gld(kmeta + 4 * tid), gld(kmeta + 4 * tid + 2)) : 0u;
   }
   MKV_DEV void put_tables() const {
     const int tid = threadIdx.x;
-    if (tid < lut_half_words(BITS) / 2) reinterpret_cast<uint4 *>(lutk)[tid] = lut4;
+    if (tid < lut_half_words(BITS) / 2) {
+      const float f = 4 * tid < lut_half_words(BITS) ? kscale : vscale;
+      const uint32_t ff = pk_f16(f, f);
+      reinterpret_cast<uint4 *>(lutk)[tid] =
+          make_uint4(pk_mul(lut4.x, ff), pk_mul(lut4.y, ff), pk_mul(lut4.z, ff), pk_mul(lut4.w, ff));
+    }
     if (tid < D / 2) tau[tid] = tau2;
   }
   MKV_DEV void fetch(int tile, Raw &r, Carry &next) const {
@@ -391,12 +404,16 @@ struct KvqLoader {
   }
   MKV_DEV void fix(int tile, const Raw &r, Tile<D> &t) const {
     const int tid = threadIdx.x;
+    const _Float16 ks = __builtin_bit_cast(h2v, scales)[0], vs = __builtin_bit_cast(h2v, scales)[1];
+    auto scaled = [](uint32_t x, _Float16 s) {
+      return __builtin_bit_cast(uint16_t, (_Float16)(__builtin_bit_cast(_Float16, (uint16_t)(x >> 16)) * s));
+    };
     auto key = [&](uint32_t e, uint32_t x) {
       const int token = (outlier_tag(x) & 31) + (e >= r.r.emid ? 32 : 0);
-      t.k[token * Tile<D>::KS + min(outlier_ch(x), D - 1)] = (uint16_t)(x >> 16);
+      t.k[token * Tile<D>::KS + min(outlier_ch(x), D - 1)] = scaled(x, ks);
     };
     auto value = [&](int token, uint32_t x) {
-      if (x != kNoOutlier) v_at(t, min(outlier_ch(x), D - 1), token >> 2)[token & 3] = (uint16_t)(x >> 16);
+      if (x != kNoOutlier) v_at(t, min(outlier_ch(x), D - 1), token >> 2)[token & 3] = scaled(x, vs);
     };
     if (r.r.e0 + tid < r.r.e1) key(r.r.e0 + tid, r.ko);
     for (uint32_t e = r.r.e0 + kTreeThreads + tid; e < r.r.e1; e += kTreeThreads) key(e, gld(kout + e));
@@ -566,6 +583,11 @@ MKV_DEV void attend_range(L &ld, Tile<D> &t, Rows<D, RB, WR> &x, int begin, int 
   }
 }
 
+MKV_DEV float uniform(float x) {  // (in a scalar register)
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
+MKV_DEV float pow2_inverse(float x) { return __builtin_bit_cast(float, 0x7F000000u - __builtin_bit_cast(uint32_t, x)); }
+
 // A weighted mean as fp16.  The weights' roundings can take it past the values it is a mean of by 2^-11: not
 // past the last finite one, which would round to infinity.
 MKV_DEV uint16_t mean_bits(float x) {
@@ -672,7 +694,7 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
   typename RowsLoader<D>::Raw nraw;
   typename RowsLoader<D>::Carry none;
   if (tree) nodes.fetch(0, nraw, none);
-  auto attend_nodes = [&]() {
+  auto attend_nodes = [&](uint32_t vscale_pair) __attribute__((always_inline)) {
     if (!tree) return;
     // A value that is infinite or NaN must reach only the rows that attend to its node: it is left out
     // of the product, where a probability of 0 would make it NaN, and added to those rows.
@@ -684,7 +706,7 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
         const uint32_t w = nraw.v[j][i];
         const uint32_t bad = ((w & 0x7C00u) == 0x7C00u ? 0xFFFFu : 0u) | ((w & 0x7C000000u) == 0x7C000000u ? 0xFFFF0000u : 0u);
         odd |= bad != 0u;
-        nraw.v[j][i] = w & ~bad;
+        nraw.v[j][i] = pk_mul(w & ~bad, vscale_pair);
       }
     nodes.put(0, nraw, tile);
     const bool any_odd = __syncthreads_or(odd);
@@ -704,13 +726,14 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
     }
     __syncthreads();
   };
+  float vscale = 1.f;  // what the outputs are times
   if (sd.method == FP16) {
     RowsLoader<D> ld;
     ld.K = reinterpret_cast<const uint16_t *>(sd.k) + h * stride_rows(sd, D);
     ld.V = reinterpret_cast<const uint16_t *>(sd.v) + h * stride_rows(sd, D);
     ld.stride = D;
     ld.n = n;
-    attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale, attend_nodes);
+    attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale, [&]() __attribute__((always_inline)) { attend_nodes(kOnePair); });
   } else if (sd.method == UQ) {
     UqLoader<D> ld;
     ld.kc = reinterpret_cast<const uint8_t *>(sd.kc) + h * stride_codes(sd);
@@ -720,7 +743,7 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
     ld.kres = reinterpret_cast<const uint16_t *>(sd.kres) + (int64_t)h * kTile * D;
     ld.meta = reinterpret_cast<uint16_t *>(s_lut);
     ld.n = n;
-    attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale, attend_nodes);
+    attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale, [&]() __attribute__((always_inline)) { attend_nodes(kOnePair); });
   } else {
     auto run = [&](auto bits_tag) {
       constexpr int BITS = decltype(bits_tag)::value;
@@ -740,7 +763,17 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
       ld.rowbytes = sd.rowbytes;
       ld.outliers = sd.bp > 0;
       ld.load_tables(cbtab, reinterpret_cast<const float *>(sd.kmeta) + (int64_t)h * D * 2);
-      attend_range<D, RB, WR>(ld, tile, x, begin, end, qscale, attend_nodes);
+      // (the drafted values are scaled as the cache's are, the keys are not: the references of their logits are
+      // before the cache's, and all of them back behind it)
+      const float kback = pow2_inverse(ld.kscale);
+      attend_range<D, RB, WR>(ld, tile, x, begin, end, uniform(qscale * kback), [&]() __attribute__((always_inline)) {
+        attend_nodes(pk_hi(ld.scales, ld.scales));
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) x.m[rb] *= ld.kscale;
+      });
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) x.m[rb] *= kback;
+      vscale = ld.vscale;
     };
     if (sd.bits == 4) run(std::integral_constant<int, 4>{});
     else if (sd.bits == 3) run(std::integral_constant<int, 3>{});
@@ -751,6 +784,7 @@ __global__ __launch_bounds__(kTreeThreads, RB == 2 ? 2 : 3) void k_tree_attn(con
   for (int rb = 0; rb < RB; ++rb) {
     x.l[rb] += __shfl_xor(x.l[rb], 16);
     x.l[rb] += __shfl_xor(x.l[rb], 32);
+    x.l[rb] *= vscale;  // (l is what o is divided by)
     x.m[rb] = __builtin_fmaf(x.m[rb], qscale, -kLift);  // from here on in log2, of what l and o are sums over
   }
   if constexpr (WT > 1) {

@@ -625,6 +625,9 @@ mkv_status mkv_cache_create(const mkv_shape *shape, const mkv_config *cfg, const
           if (i > 0 && !(x >= src[half * nc + i - 1])) return fail(MKV_EINVAL, "codebooks must be ascending");
           dst[half * nc + i] = x;
         }
+        float scale = 1.f;
+        while (std::max(-src[half * nc], src[half * nc + nc - 1]) * scale > 1.f) scale *= 0.5f;
+        table[cb_scale(b) + half] = scale;
         for (int i = 0; i + 1 < nc; ++i) {
           volatile float sum = src[half * nc + i] + src[half * nc + i + 1];
           dst[2 * nc + half * (nc - 1) + i] = sum * 0.5f;

@@ -112,6 +112,10 @@ __host__ __device__ inline int cb_offset(int bits) {
   return bits == 2 ? 0 : bits == 3 ? 14 : 44;
 }
 constexpr int kCbTableFloats = 14 + 30 + 62;
+// Behind it, for b = 2, 3, 4 the key's and the value's power of two (at most 1) that takes the codebook's
+// largest magnitude to 1 or less: what a code stands for, up to that magnitude times fp16's last finite value,
+// is an fp16 value after it.
+__host__ __device__ inline int cb_scale(int bits) { return kCbTableFloats + 2 * (bits - 2); }
 
 // Lookup tables of the KVQ codebooks for the attention, built on the host at cache creation and
 // stored after the codebook table (kLutBase floats into the same device region): for b = 2 one

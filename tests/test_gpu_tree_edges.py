@@ -245,3 +245,49 @@ def test_one_weight_rounded_up_takes_no_value_past_the_end():
     mask = (np.uint64(1) << np.arange(n, dtype=np.uint64))[None]
     got = attend(c, q, kt, np.full((1, n, hkv, d), 65504.0, np.float16), mask).astype(np.float64)
     assert np.all(np.abs(got - 65504) <= 2 * U * 65504), got.max()
+
+
+def ratio_books(key, value):
+    """Codebooks for 2, 3 and 4 bits whose largest entries are `key` and `value`: {bits: (keys, values)}, flat."""
+    books = {b: tuple((np.linspace(-1, 1, 1 << b) * top).astype(np.float16).astype(np.float32) for top in (key, value))
+             for b in (2, 3, 4)}
+    return books, [float(x) for b in (2, 3, 4) for cb in books[b] for x in cb]
+
+
+@pytest.mark.parametrize("key,value", [(1.0, 1.0), (1.0625, 1.1875), (3.0, 2.5), (0.5, 1.5), (700.0, 1.0)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_kvquant_thresholds_at_the_end_of_fp16(d, key, value):
+    """Codebooks that go past their thresholds (an entry of 1.19 stands for 1.19 times it) and thresholds and
+    scales up to the last finite fp16 value: what a code stands for may then lie past fp16's end."""
+    from oracle.sequence import Sequence
+    from paper_2609_07966_amd.cache import KVCache
+    rng = np.random.default_rng(36)
+    lens, hq, hkv, n = [90, 300, 1100], 4, 2, 6
+    cfgs = [{"method": "kvq", "bits": b, "outlier_bp": bp} for b, bp in ((4, 100), (3, 400), (2, 0))]
+    books, flat = ratio_books(key, value)
+    t = sum(lens)
+    k, v = (rng.standard_normal((t, hkv, d)).astype(np.float16) for _ in range(2))
+    # tokens of all sizes, a third of them up to the last finite value; four channels of such keys
+    size = np.where(rng.random((t, hkv, 1)) < 1 / 3, 65504.0, 10.0 ** rng.integers(-2, 4, (t, hkv, 1)))
+    v = (rng.uniform(-1, 1, (t, hkv, d)) * size).astype(np.float16)
+    v[0] = 65504
+    k[..., :4] = (rng.uniform(-1, 1, (t, hkv, 4)) * 65504).astype(np.float16)
+    c = KVCache((3, hq, hkv, d, 4), cfgs, lens, codebooks=flat)
+    c.append_prompt(dev(k), dev(v))
+    q, kt, vt = (rng.standard_normal((3, n, h, d)).astype(np.float16) for h in (hq, hkv, hkv))
+    q = (q / max(1.0, key)).astype(np.float16)
+    q[..., :4] = (rng.standard_normal((3, n, hq, 4)) * 2.0 ** -13 / max(1.0, key)).astype(np.float16)
+    mask, _ = trees(rng, 3, n)
+    mask[:, 0] = 0
+    got = attend(c, q, kt, vt, mask).astype(np.float64)
+    row = past = 0
+    for s, n0 in enumerate(lens):
+        seq = Sequence(cfgs[s], k[row:row + n0], v[row:row + n0], hq, codebooks=books)
+        keys, vals = [x["eff"] for x in seq.kq], [x["eff"] for x in seq.vq]
+        # a decoded value's own rounding; near 0 half a subnormal step, of values in units of the codebook's largest
+        # entry (a power of two at most twice it)
+        err = lambda x, top: U * np.abs(x) + 2.0 ** -25 * max(1.0, 2 * top)
+        past += sum(float(np.abs(x).max()) > 65520 for x in vals)
+        bounded(keys, vals, [err(x, key) for x in keys], [err(x, value) for x in vals], q[s], kt[s], vt[s], mask[s], got[s])
+        row += n0
+    assert value <= 1 or past > 0
