@@ -437,10 +437,11 @@ mkv_status mkv_tree_attention(mkv_cache *cache, const uint16_t *q, const uint16_
  *   path    device int32 [S][max_path]; an entry outside 0..n_nodes-1 ends the sequence's path
  *   n_path  device int32 [S], clamped to 0..max_path; 0 accepts nothing
  *   counts  optional device int32 [S]: the tokens that each sequence then holds (its kv heads hold
- *           the same tokens)
+ *           the same ones, unless decode steps were replayed past max_new_tokens)
  * The same caches and call order as mkv_tree_attention; max_path >= 1.  How many tokens were
- * accepted is known to the device alone, so capacity is checked there as for replayed steps: a token
- * that finds its region full is dropped, and mkv_decode_step's own count of steps does not move.
+ * accepted is known to the device alone, so capacity is checked there: a sequence that holds its prompt
+ * and max_new_tokens more, under whichever method, drops further ones, and mkv_decode_step's own count
+ * of steps does not move.
  * One launch; may be captured.
  */
 mkv_status mkv_tree_accept(mkv_cache *cache, const uint16_t *k, const uint16_t *v, int32_t n_nodes,

@@ -966,7 +966,7 @@ __global__ __launch_bounds__(64 * kAcceptWaves) void k_tree_accept(const SeqDesc
                                                                    const float *__restrict__ cbtab, int Hkv, int n_nodes,
                                                                    const int32_t *__restrict__ path,
                                                                    const int32_t *__restrict__ n_path, int max_path,
-                                                                   int32_t *counts) {
+                                                                   int max_new, int32_t *counts) {
   constexpr int CH = D / 64, NT = 64 * kAcceptWaves;
   __shared__ AcceptLds<D> L;
   const int seq = blockIdx.x / Hkv, h = blockIdx.x % Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -992,7 +992,10 @@ __global__ __launch_bounds__(64 * kAcceptWaves) void k_tree_accept(const SeqDesc
   __syncthreads();
   // the open value block goes on (its words by the threads that store them below)
   if (tid < words && (count & 3) != 0) L.blk[0][tid] = gld(blocks + (int64_t)(count >> 2) * words + tid);
-  const int take = min(L.take, cap - count);
+  // (a method may have room for up to three tokens more, where it rounds its capacity up: they are not taken,
+  // so that equal paths leave equal counts.  Up to there the outlier pools have room for every channel of every
+  // token: the heads of a sequence hold the same tokens)
+  const int take = min(L.take, min(cap, sd.n0 + max_new) - count);
   float2 tau[CH];
 #pragma unroll
   for (int i = 0; i < CH; ++i) tau[i] = method == KVQ ? kvq_key_tau(sd, h, lane + 64 * i, D) : make_float2(0.f, 0.f);
@@ -1182,7 +1185,7 @@ hipError_t launch_tree_accept(const Dev &dv, const Shape &sh, const uint16_t *k,
                               const int32_t *path, const int32_t *n_path, int max_path, int32_t *counts, hipStream_t st) {
   auto kernel = sh.D == 64 ? k_tree_accept<64> : k_tree_accept<128>;
   hipLaunchKernelGGL(kernel, dim3(sh.S * sh.Hkv), dim3(64 * kAcceptWaves), 0, st, dv.seqs, dv.state, k, v, dv.cbtab, sh.Hkv, n_nodes,
-                     path, n_path, max_path, counts);
+                     path, n_path, max_path, sh.max_new, counts);
   return hipGetLastError();
 }
 

@@ -3,7 +3,7 @@ at the end of fp16's range, full caches, and decode steps after an acceptance.""
 import numpy as np
 import pytest
 
-from test_gpu_tree import Held, U, admitted, check, dev, drafts, trees, workload
+from test_gpu_tree import CONFIGS, Held, U, admitted, check, dev, drafts, exports, same_state, trees, workload
 
 pytestmark = pytest.mark.gpu
 
@@ -291,3 +291,34 @@ def test_kvquant_thresholds_at_the_end_of_fp16(d, key, value):
         bounded(keys, vals, [err(x, key) for x in keys], [err(x, value) for x in vals], q[s], kt[s], vt[s], mask[s], got[s])
         row += n0
     assert value <= 1 or past > 0
+
+
+# ---- acceptance ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("max_new", [1, 5, 6, 7, 8])
+def test_accept_ends_at_max_new_under_every_method(d, max_new):
+    """Equal paths leave equal numbers of tokens in a mixed batch, whatever their methods round their room
+    up to, in one acceptance or over several; and every kv head holds them."""
+    import torch
+    names, n0 = CONFIGS + ["KVQ4"], 61
+    wl = workload(names, [n0] * 6, 4, 2, d)
+    cfg = wl.cfg
+    wl.cfg = lambda s: dict(cfg(s), outlier_bp=5000) if s == 5 else cfg(s)
+    rng = np.random.default_rng(37)
+    _, kt, vt = drafts(wl, rng, 12)
+    kt *= 50  # (nearly every key past its threshold: the outlier pools fill up)
+    path = np.tile(np.arange(12, dtype=np.int32), (6, 1))
+    counts = torch.zeros(6, dtype=torch.int32, device="cuda")
+    state = []
+    for rounds in ([12], [2, 3, 12, 12]):
+        c, _ = admitted(wl, max_new)
+        at = 0
+        for m in rounds:
+            c.tree_accept(dev(kt), dev(vt), dev(np.roll(path, -at, 1)), dev(np.full(6, m, np.int32)), counts)
+            at = min(at + m, max_new)
+            assert counts.tolist() == [n0 + at] * 6
+        assert at == max_new
+        assert all(c.counts(s, h)[0] == n0 + max_new for s in range(6) for h in range(2))
+        state.append([exports(c, s, h, wl.cfg(s)["method"]) for s in range(6) for h in range(2)])
+    assert all(same_state(a, b) for a, b in zip(*state))
