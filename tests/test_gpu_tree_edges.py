@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 
 from test_gpu_tree import CONFIGS, Held, U, admitted, check, dev, drafts, exports, same_state, trees, workload
+from workloads import step_inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -322,3 +323,47 @@ def test_accept_ends_at_max_new_under_every_method(d, max_new):
         assert all(c.counts(s, h)[0] == n0 + max_new for s in range(6) for h in range(2))
         state.append([exports(c, s, h, wl.cfg(s)["method"]) for s in range(6) for h in range(2)])
     assert all(same_state(a, b) for a, b in zip(*state))
+
+
+def configured(names, extra, lens, hq, hkv, d):
+    wl = workload(names, lens, hq, hkv, d)
+    cfg = wl.cfg
+    wl.cfg = lambda s: {"method": "kvq", "bits": extra[s][0], "outlier_bp": extra[s][1]} if s in extra else cfg(s)
+    return wl
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_decode_steps_after_an_acceptance(d):
+    """The decode step reads what acceptance wrote through other words than the tree attention does (an
+    outlier's difference from its code): steps after it are bit for bit those of a twin that appended the same
+    tokens one decode step at a time, with several outliers a token, fewer than there are slots for, and none.
+    The first beam of each pair accepts over slots that held other tokens before it took the second's state."""
+    import torch
+    each = CONFIGS + ["KVQ4"] * 4
+    extra = {5: (4, 400), 6: (3, 250), 7: (2, 5000), 8: (4, 0)}
+    lens = [70, 60, 50, 33, 126, 90, 65, 40, 64]
+    wl = configured([x for x in each for _ in range(2)], {2 * i + w: x for i, x in extra.items() for w in range(2)},
+                    [x for x in lens for _ in range(2)], 8, 2, d)
+    s, n, m = wl.n_seqs, 10, 7
+    rng = np.random.default_rng(38)
+    q, kt, vt = drafts(wl, rng, n)
+    vt[:, 4, :, : d // 2] = 0
+    vt[:, 5] = 1  # ties: nothing over the scale
+    kt[:, 6] *= 30
+    path = np.tile(np.array([6, 4, 0, 5, 9, 4, 2], np.int32), (s, 1))
+    a, _ = admitted(wl, 24, same=2)
+    b, _ = admitted(wl, 24, same=2)
+    a.tree_accept(dev((kt * -3).astype(np.float16)), dev((vt[:, ::-1] * 5).astype(np.float16)), dev(path),
+                  dev(np.tile(np.array([m, 0], np.int32), s // 2)))
+    a.reorder(dev(np.ones(s, np.int32)), 2)
+    a.tree_accept(dev(kt), dev(vt), dev(path), dev(np.full(s, m, np.int32)))
+    out_a, out_b = (torch.empty((s, 8, d), dtype=torch.float32, device="cuda") for _ in range(2))
+    for node in path[0]:
+        b.step(dev(kt[:, node]), dev(vt[:, node]), dev(q[:, 0]), out_b)
+    for t in range(4):
+        one = [dev(x) for x in step_inputs(wl, t)]
+        a.step(*one, out_a)
+        b.step(*one, out_b)
+        assert bool(torch.isfinite(out_a).all())
+        for i in range(s):
+            assert torch.equal(out_a[i], out_b[i]), (t, i, wl.cfg(i))
