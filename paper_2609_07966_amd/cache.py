@@ -39,6 +39,11 @@ class KVCache:
     shape: (n_seqs, n_q_heads, n_kv_heads, head_dim, max_new_tokens)
     cfgs:  per-sequence configuration dicts (workloads.configs rows)
     codebooks: flat 56 float32 values (b = 2, 3, 4: key then value codebook), or None
+
+    Every call enqueues on the stream the cache was made with (`stream`, or the one current then).  The prefill
+    and decode calls do no more: whoever makes their inputs or reads their outputs on another stream orders
+    the two.  tree_attention, tree_accept and reorder, which go with the calls of `decoding` on the current
+    stream, are ordered with the current stream where it is another one.
     """
 
     def __init__(self, shape, cfgs, prompt_lens, codebooks=None, device="cuda", stream=None):
@@ -114,8 +119,8 @@ class KVCache:
         """Attention of drafted nodes over the cache and each other -> out [S][N][Hq][D] fp16.
 
         q [S][N][Hq][D], k, v [S][N][Hkv][D] fp16; mask [S][N] int64, bit j of a node's word = it
-        attends to node j; n_valid: optional int32 [S], the nodes each sequence has.  The default
-        workspace is allocated for the call, on the cache's stream."""
+        attends to node j; n_valid: optional int32 [S], the nodes each sequence has (rows of others stay as
+        they are in `out`, and undefined without one).  The default workspace is allocated for the call."""
         torch, dev = self.torch, self.arena.device
         n = q.shape[1] if q.dim() == 4 else 0
         check_tensor("q", q, dev, torch.float16, (self.S, n, self.Hq, self.D))
@@ -129,28 +134,32 @@ class KVCache:
         ws = workspace
         if ws is not None:
             check_workspace(ws, dev)
-        if out is None or ws is None:
-            # memory allocated here belongs to the cache's stream
-            if raw_stream(dev) == self.s:
-                out, ws = self._tree_buffers(q, n, out, ws)
-            else:
-                with torch.cuda.stream(self.stream):
-                    out, ws = self._tree_buffers(q, n, out, ws)
+        # (allocated on the current stream, whose further work comes behind the call)
+        if out is None:
+            out = torch.empty_like(q)
+        if ws is None:
+            ws = self.tree_workspace(n)
         self._launch(L.mkv_tree_attention, _ptr(q), _ptr(k), _ptr(v), _ptr(mask), _ptr(n_valid), n, _ptr(out), _ptr(ws),
                      ws.numel())
         return out
 
     def _launch(self, fn, *args):
-        """fn(handle, *args, stream) with the cache's device current."""
+        """fn(handle, *args, stream) with the cache's device current.  Where another stream than the cache's is
+        current, the call comes behind that stream's work, and its further work behind the call: tensors
+        written, read or freed there need no care."""
         device = self.arena.device
-        if self.torch.cuda.current_device() == device.index:
+        if self.torch.cuda.current_device() != device.index:
+            with self.torch.cuda.device(device):
+                return self._launch(fn, *args)
+        if raw_stream(device) == self.s:
             fn(self.h, *args, self.s)
         else:
-            with self.torch.cuda.device(device):
+            current = self.torch.cuda.current_stream(device)
+            self.stream.wait_stream(current)
+            try:
                 fn(self.h, *args, self.s)
-
-    def _tree_buffers(self, q, n, out, ws):
-        return self.torch.empty_like(q) if out is None else out, self.tree_workspace(n) if ws is None else ws
+            finally:  # (a stream that has joined a capture has to come back, also from a refused call)
+                current.wait_stream(self.stream)
 
     def tree_accept(self, k, v, path, n_path, counts=None):
         """Append nodes path[s][:n_path[s]] of k, v [S][N][Hkv][D] to each sequence; path [S][M], n_path [S]

@@ -367,3 +367,119 @@ def test_decode_steps_after_an_acceptance(d):
         assert bool(torch.isfinite(out_a).all())
         for i in range(s):
             assert torch.equal(out_a[i], out_b[i]), (t, i, wl.cfg(i))
+
+
+# ---- streams ---------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("side", [True, False])
+def test_cache_calls_follow_the_current_stream(side):
+    """rope and beam_select run on the current stream and the cache's calls on the stream it was made with:
+    with two different ones, inputs still on their way and outputs read at once, a round gives what it gives
+    on one stream."""
+    import torch
+    from paper_2609_07966_amd import decoding
+    wl = workload(["FP16", "FP16", "KVQ4", "KVQ4", "UQ4-g64", "UQ4-g64"], [200, 200, 90, 90, 150, 150], 8, 2, 128)
+    s, n, m = 6, 8, 3
+    rng = np.random.default_rng(39)
+    inv_freq = dev((10000.0 ** (-np.arange(64) / 64)).astype(np.float32))
+    rounds = []
+    for _ in range(3):
+        q, kt, vt = drafts(wl, rng, n)
+        mask, _ = trees(rng, s, n)
+        rounds.append([dev(x) for x in (q, kt, vt, mask.view(np.int64), np.tile(rng.integers(0, 1000, n), s)[None].astype(np.int32),
+                                        rng.integers(0, n, (s, m)).astype(np.int32), rng.integers(0, m + 1, s).astype(np.int32),
+                                        rng.standard_normal((s // 2, 2, 4001)).astype(np.float32))])
+    scores = torch.zeros((s // 2, 2), device="cuda")
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def go(c, slow):
+        results = []
+        for x in rounds:
+            held = [torch.zeros_like(t) for t in x]
+            if slow:
+                torch.cuda._sleep(4000000)  # some ms, before the inputs are there
+            for dst, src in zip(held, x):
+                dst.copy_(src)
+            q, kt, vt, mask, pos, path, n_path, logits = held
+            qr, kr = decoding.rope([q.view(s * n, 8, 128), kt.view(s * n, 2, 128)], pos, inv_freq)
+            qr, kr = qr.view(q.shape), kr.view(kt.shape)
+            out = c.tree_attention(qr, kr, vt, mask)
+            results.append(out * 1)  # (read at once, on the current stream)
+            counts = torch.zeros(s, dtype=torch.int32, device="cuda")
+            c.tree_accept(kr, vt, path, n_path, counts)
+            results.append(counts * 1)
+            _, parent, _ = decoding.beam_select(logits, scores, 2)
+            c.reorder(parent.view(-1), 2)
+            del held, q, kt, vt, mask, qr, kr, out, parent
+        return results
+
+    with torch.cuda.stream(a):
+        one, _ = admitted(wl, 40, same=2, stream=a)
+        want = go(one, False)
+    torch.cuda.synchronize()
+    two, _ = admitted(wl, 40, same=2, stream=a if side else torch.cuda.default_stream())
+    torch.cuda.synchronize()
+    with torch.cuda.stream(b):
+        got = go(two, True)
+    torch.cuda.synchronize()
+    for x, y in zip(want, got):
+        assert torch.equal(x, y)
+    for i in range(s):
+        for h in range(2):
+            assert same_state(exports(one, i, h, wl.cfg(i)["method"]), exports(two, i, h, wl.cfg(i)["method"]))
+
+
+def test_cache_calls_captured_on_another_stream():
+    """Captured under a stream that is not the cache's: the cache's stream joins the capture and comes back."""
+    import torch
+    wl = workload(["FP16", "KVQ3", "UQ4-g64"], [300, 90, 150], 8, 2, 64)
+    rng = np.random.default_rng(40)
+    q, kt, vt = drafts(wl, rng, 6)
+    mask, _ = trees(rng, 3, 6)
+    inputs = [dev(x) for x in (q, kt, vt, mask.view(np.int64))]
+    path, n_path = dev(np.tile(np.arange(6, dtype=np.int32), (3, 1))), dev(np.array([2, 0, 3], np.int32))
+    own, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(own):
+        eager, _ = admitted(wl, 40, stream=own)
+        twin, _ = admitted(wl, 40, stream=own)
+    torch.cuda.synchronize()
+    out = torch.zeros_like(inputs[0])
+    ws = eager.tree_workspace(6)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=other):
+        twin.tree_attention(*inputs, out=out, workspace=ws)
+        twin.tree_accept(inputs[1], inputs[2], path, n_path)
+    for _ in range(4):
+        want = eager.tree_attention(*inputs)
+        eager.tree_accept(inputs[1], inputs[2], path, n_path)
+        torch.cuda.synchronize()
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    for i in range(3):
+        assert same_state(exports(eager, i, 1, wl.cfg(i)["method"]), exports(twin, i, 1, wl.cfg(i)["method"]))
+
+
+def test_a_refused_call_leaves_a_capture_whole():
+    import torch
+    from paper_2609_07966_amd import _lib
+    wl = workload(["FP16"], [100], 4, 2, 64)
+    rng = np.random.default_rng(41)
+    q, kt, vt = drafts(wl, rng, 4)
+    inputs = [dev(x) for x in (q, kt, vt, np.ones((1, 4), np.int64))]
+    own, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(own):
+        c, _ = admitted(wl, 4, stream=own)
+        want = c.tree_attention(*inputs)
+    torch.cuda.synchronize()
+    out = torch.zeros_like(want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=other):
+        with pytest.raises(_lib.MkvError):
+            c.reorder(torch.zeros(1, dtype=torch.int32, device="cuda"), 33)
+        c.tree_attention(*inputs, out=out)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
