@@ -1,7 +1,8 @@
 // Beam selection: the best continuations of every request's beams.
 //
 // A continuation (w, t) scores scores[w] + logit(w, t) - lse(w).  Within a beam that order is the
-// logits' own, so one pass over the logits is enough: each workgroup takes a chunk of one beam's
+// logits' own (but for scores that are equal though the logits are not, see take_ties), so one pass over the
+// logits is enough: each workgroup takes a chunk of one beam's
 // vocabulary into registers and writes the chunk's best n_select logits, its maximum and its sum of
 // exponentials; a second, small launch has every request's candidates compared by their full scores
 // in float64 (two beams' scores lie closer than float32 tells apart once in some thousand selections).
@@ -228,9 +229,71 @@ MKV_DEV Rank row_best(Rank x) {
   return x;
 }
 
+// Where the K-th score is shared by continuations that no chunk listed, which one is taken is the lower index's,
+// not the larger logit's: scores of 64 bits so far from 0 that a logit changes nothing (dead beams given
+// the lowest finite score), or logits that small.  A chunk can hide such a one only if the last it listed ties
+// too: its logits are gone through again, in the order of the indexes, with what the other chunks listed.
+// For the whole workgroup; `need` outputs, which exist, go to write(i, rank) for i < need.
+template <typename CandOf, typename Write>
+MKV_DEV void take_ties(const BeamArgs &a, u64 score, int need, int n_chunks, int chunk, const double *s_base, const int *s_done,
+                       int *s_counts, CandOf cand_of, Write write) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = a.n_select, b = blockIdx.x;
+  const uint64_t below = (1ull << lane) - 1;
+  int got = 0;
+  for (int w = 0; w < a.n_beams && got < need; ++w) {
+    const double base = s_base[w];
+    const u64 index = (u64)w * a.vocab;
+    if (s_done[w]) {
+      if (double_key(base) == score) {
+        if (tid == 0) write(got, Rank{score, index + a.pad_token});
+        ++got;
+      }
+      continue;
+    }
+    auto ties = [&](double logit) { return double_key(base + logit) == score; };
+    for (int c = 0; c < n_chunks && got < need; ++c) {
+      const int first = (w * n_chunks + c) * K;
+      const BeamCandidate top = cand_of(first), last = cand_of(first + K - 1);
+      if (top.token < 0 || double_key(base + (double)top.logit) < score) continue;
+      if (last.token >= 0 && ties((double)last.logit)) {
+        const int end = min(a.vocab, (c + 1) * chunk);
+        for (int t0 = c * chunk; t0 < end && got < need; t0 += kMergeThreads) {
+          const int t = t0 + tid;
+          const int64_t at = ((int64_t)b * a.n_beams + w) * a.row_stride + t;
+          bool hit = false;
+          if (t < end)
+            hit = ties(a.half ? h2f(gld(static_cast<const uint16_t *>(a.logits) + at)) : gld(static_cast<const float *>(a.logits) + at));
+          const uint64_t hits = __ballot(hit);
+          if (lane == 0) s_counts[wave] = __popcll(hits);
+          __syncthreads();
+          int before = 0, all = 0;
+          for (int i = 0; i < kMergeWaves; ++i) {
+            before += i < wave ? s_counts[i] : 0;
+            all += s_counts[i];
+          }
+          const int place = got + before + __popcll(hits & below);
+          if (hit && place < need) write(place, Rank{score, index + t});
+          got += all;
+          __syncthreads();
+        }
+      } else {  // (at most 64 listed, best first: every wave looks at them, the first one writes)
+        const BeamCandidate mine = cand_of(first + min(lane, K - 1));
+        const bool hit = lane < K && mine.token >= 0 && ties((double)mine.logit);
+        uint64_t rest = __ballot(hit);
+        const int all = __popcll(rest);
+        int place = got;
+        for (; rest; rest &= rest - 1) place += __shfl(mine.token, __builtin_ctzll(rest)) < mine.token ? 1 : 0;
+        if (wave == 0 && hit && place < need) write(place, Rank{score, index + mine.token});
+        got += all;
+      }
+    }
+  }
+}
+
 // One workgroup per request.
 __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a, const BeamPartial *__restrict__ parts,
-                                                             const BeamCandidate *__restrict__ cands, int n_chunks) {
+                                                             const BeamCandidate *__restrict__ cands, int n_chunks,
+                                                             int chunk) {
   __shared__ double s_base[MKV_BEAM_MAX];  // scores[w] - lse(w); a finished beam: scores[w]
   __shared__ int s_done[MKV_BEAM_MAX];
   __shared__ Rank s_group[kBeamGroups];
@@ -238,7 +301,11 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a, const 
   __shared__ __attribute__((aligned(16))) uint32_t s_group32[kBeamGroups];
   __shared__ uint32_t s_tau;
   __shared__ int s_n;
+  __shared__ u64 s_edge;  // the best score that a chunk listed last: it may have more of that one
+  __shared__ int s_over;  // outputs above it
+  __shared__ int s_counts[kMergeWaves];
   constexpr int kCap = kListCap / 2, kAhead = 2;
+  static_assert(kCap <= kMergeThreads, "a thread for every one listed");
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int b = blockIdx.x, W = a.n_beams, K = a.n_select;
   const int per = n_chunks * K, total = W * per;
@@ -247,6 +314,8 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a, const 
   BeamCandidate mine[kAhead];
 #pragma unroll
   for (int u = 0; u < kAhead; ++u) mine[u] = cand_of(min(tid + u * kMergeThreads, total - 1));
+  const int lists = W * n_chunks;
+  const BeamCandidate final = cand_of(min(tid, lists - 1) * K + K - 1);
   auto rank = [&](int i, const BeamCandidate &c) {
     const int w = i / per;
     if (s_done[w])
@@ -254,7 +323,10 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a, const 
     if (c.token < 0) return Rank{0, ~0ull};
     return Rank{double_key(s_base[w] + (double)c.logit), (u64)w * a.vocab + c.token};
   };
-  if (tid == 0) s_n = 0;
+  if (tid == 0) {
+    s_n = s_over = 0;
+    s_edge = 0;
+  }
   for (int w = wave; w < W; w += kMergeWaves) {
     const int64_t row = (int64_t)b * W + w;
     float m = -INFINITY;
@@ -287,6 +359,14 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a, const 
     const Rank r = rank_of(i);
     if (above(r, best)) best = r;
   }
+  u64 edge = 0;
+  for (int l = tid; l < lists; l += kMergeThreads) {
+    const BeamCandidate c = l == tid ? final : cand_of(l * K + K - 1);
+    const int w = l / n_chunks;
+    if (!s_done[w] && c.token >= 0) edge = max(edge, double_key(s_base[w] + (double)c.logit));
+  }
+  edge = group8_max(edge);
+  if ((lane & 7) == 0 && edge != 0) atomicMax(&s_edge, edge);
   // the K-th best group by the upper half of its score
   const uint32_t gm = group_max<16>((uint32_t)(best.score >> 32));
   if ((lane & 15) == 0) s_group32[tid >> 4] = gm;
@@ -297,8 +377,10 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a, const 
   }
   __syncthreads();
   const uint32_t tau = s_tau;
+  const u64 last_listed = s_edge;
   auto collect = [&](const Rank &r) {
     if (r.score == 0 || (uint32_t)(r.score >> 32) < tau) return;
+    if (r.score > last_listed) atomicAdd(&s_over, 1);
     const int at = atomicAdd(&s_n, 1);
     if (at < kCap) s_list[at] = r;
   };
@@ -315,17 +397,19 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a, const 
     a.parent[o] = r.score ? (int)(r.index / a.vocab) : 0;
     a.score_out[o] = r.score ? (float)key_double(r.score) : -INFINITY;
   };
+  // (no chunk's last score is above the K-th: with fewer than K above it, it is the K-th)
+  const int over = last_listed != 0 && s_over < K ? s_over : K;
   if (n <= kCap) {
-    for (int i = tid; i < n; i += kMergeThreads) {
-      const Rank mine = s_list[i];
+    if (tid < n) {
+      const Rank mine = s_list[tid];
       int before = 0;
       for (int j = 0; j < n; ++j) before += above(s_list[j], mine) ? 1 : 0;
-      if (before < K) write(before, mine);
+      if (before < over) write(before, mine);
     }
-    if (tid < K && tid >= n) write(tid, Rank{0, 0});
+    if (tid < over && tid >= n) write(tid, Rank{0, 0});
   } else {
     Rank last = {~0ull, 0};
-    for (int r = 0; r < K; ++r) {
+    for (int r = 0; r < over; ++r) {
       Rank top = {0, ~0ull};
       for (int i = tid; i < total; i += kMergeThreads) {
         const Rank c = rank_of(i);
@@ -342,6 +426,8 @@ __global__ __launch_bounds__(kMergeThreads) void k_beam_merge(BeamArgs a, const 
       if (tid == 0) write(r, all);
     }
   }
+  if (over < K)
+    take_ties(a, last_listed, K - over, n_chunks, chunk, s_base, s_done, s_counts, cand_of, [&](int i, const Rank &r) { write(over + i, r); });
 }
 
 template <typename T>
@@ -354,7 +440,8 @@ hipError_t beam_impl(const BeamArgs &a, hipStream_t st) {
                      static_cast<const T *>(a.logits), a.row_stride, a.vocab, a.n_select, chunks, parts, cands);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_beam_merge, dim3(a.n_batch), dim3(kMergeThreads), 0, st, a, parts, cands, chunks);
+  hipLaunchKernelGGL(k_beam_merge, dim3(a.n_batch), dim3(kMergeThreads), 0, st, a, parts, cands, chunks,
+                     kScanThreads * beam_values(rows, a.vocab));
   return hipGetLastError();
 }
 

@@ -331,3 +331,36 @@ def test_beam_refusals():
         decoding.beam_select(x, s, 3, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert e.value.status == 2
     assert decoding.beam_select(x[:0], s[:0], 3)[0].shape == (0, 3)
+
+
+@pytest.mark.parametrize("dtype", [np.float32, np.float16])
+@pytest.mark.parametrize("w,v,k", [(4, 40000, 8), (3, 1000, 64), (1, 20000, 2), (32, 9000, 64)])
+def test_beam_ties_of_scores_whose_logits_differ(w, v, k, dtype):
+    """Scores so far from 0 that adding a logit's log-probability changes nothing, as where dead beams are
+    given the lowest finite score: continuations tie though their logits do not, and the lower index goes
+    first, past what the largest logits would be."""
+    rng = np.random.default_rng(8)
+    logits = (rng.standard_normal((4, w, v)) * 3).astype(dtype)
+    logits[2, :, ::3] = -np.inf
+    logits[3, :, :v - k // 2 - 1] = -np.inf
+    scores = np.full((4, w), np.finfo(np.float32).min, np.float32)
+    scores[1] = -1e30
+    scores[1, w // 2] = -2.0                   # one live beam
+    finished = np.zeros((4, w), np.uint8)
+    if w > 1:
+        scores[0, 0] = -3.0                    # finished: one continuation, then the ties of the others
+        finished[0, 0] = 1
+        finished[1, w - 1] = 1
+        finished[2, 1] = 1                     # a tie among the ties
+    for f in (None, finished):
+        agree(select(logits, scores, k, f, pad=7), best(logits, scores, k, f, pad=7))
+
+
+def test_beam_ties_of_sums():
+    """Logits too small to change their beam's score in 64 bits."""
+    rng = np.random.default_rng(9)
+    logits = (rng.random((2, 3, 30000)) * 1e-19).astype(np.float32)
+    logits[1, :, 20000:] = 2.5                  # some above them
+    logits[1, :, 20004:] = -1.0
+    scores = np.array([[-2.0, -2.0, -2.5], [-1.0, -1.0, -1.0]], np.float32)
+    agree(select(logits, scores, 12), best(logits, scores, 12))
