@@ -415,12 +415,21 @@ mkv_status mkv_rope(const mkv_rope_spec *spec, const float *inv_freq, const int3
  *              nodes that do not exist are ignored; a word of 0 leaves the cached tokens)
  *   n_valid    optional device int32 [S]: sequence s has only its first n_valid[s] nodes (clamped to
  *              0..n_nodes); the others are not read and their rows of `out` stay as they were
- *   out        device fp16 [S][n_nodes][Hq][d]; sums and softmax in 32 bits, rounded once; may not
- *              overlap an input
+ *   out        device fp16 [S][n_nodes][Hq][d]; may not overlap an input
  *   workspace  device, >= mkv_tree_workspace(cache, n_nodes) bytes, 256-byte aligned, used until the
  *              call's work is done: calls that may overlap need one each.  NULL if 0 bytes are needed.
  * n_nodes is 1..MKV_TREE_MAX_NODES.  After prefill or a completed decode step; changes no state of
  * the cache.  One launch or two; may be captured (counts are read on the device).
+ *
+ * Sums, maxima and softmax statistics are held in 32 bits and the result is rounded to fp16 once, but the
+ * products take fp16 operands, to which the probabilities and the keys and values that codes stand for
+ * are rounded (stored fp16 rows and outliers are exact).  A quantized cache's rows are therefore less exact
+ * than mkv_decode_attention's, whose keys and values stay in more bits: on 4000 tokens whose keys have two
+ * channels of 8 times the size, the error against 64 bits (2-norm, relative) is 3e-4 to 6.5e-4 under KVQ
+ * and 6e-4 to 1.1e-3 under UQ, where the step's is 0.5e-4 to 0.8e-4 and 5e-4 to 6e-4; fp16 caches 2.2e-4, of
+ * which the result's own rounding is 2.1e-4.
+ * A NaN or infinity in a node's key or value reaches the rows that attend to the node and no others.  A
+ * mean of finite fp16 values is finite.
  */
 #define MKV_TREE_MAX_NODES 64
 
@@ -437,7 +446,7 @@ mkv_status mkv_tree_attention(mkv_cache *cache, const uint16_t *q, const uint16_
  *   path    device int32 [S][max_path]; an entry outside 0..n_nodes-1 ends the sequence's path
  *   n_path  device int32 [S], clamped to 0..max_path; 0 accepts nothing
  *   counts  optional device int32 [S]: the tokens that each sequence then holds (its kv heads hold
- *           the same ones, unless decode steps were replayed past max_new_tokens)
+ *           the same ones, unless decode steps went past max_new_tokens)
  * The same caches and call order as mkv_tree_attention; max_path >= 1.  How many tokens were
  * accepted is known to the device alone, so capacity is checked there: a sequence that holds its prompt
  * and max_new_tokens more, under whichever method, drops further ones, and mkv_decode_step's own count
@@ -453,11 +462,11 @@ mkv_status mkv_tree_accept(mkv_cache *cache, const uint16_t *k, const uint16_t *
  * (w, t) of beam w by token t has the score
  *   scores[b][w] + logits[b][w][t] - log sum_u exp(logits[b][w][u])
  * and a finished beam has one continuation, (w, pad_token), with its score unchanged.  Scores are
- * formed and compared in 64 bits (the exponentials under the logarithm in 32, their sum in 64); ties
- * go to the lower w * vocab + t.  A NaN logit counts as -infinity, and a continuation whose score is
- * not above -infinity (a dead beam's, a banned token's, or NaN) is never chosen: where fewer than
- * n_select are left, the last outputs are (parent 0, pad_token) with the score -infinity.  (A +infinity
- * logit makes every score of its beam NaN.)
+ * formed and compared in 64 bits (the exponentials under the logarithm in 32, summed in 32 over 16 of them
+ * at most and in 64 from there on); ties go to the lower w * vocab + t.  A NaN logit counts as
+ * -infinity, and a continuation whose score is not above -infinity (a dead beam's, a banned token's, or
+ * NaN) is never chosen: where fewer than n_select are left, the last outputs are (parent 0, pad_token)
+ * with the score -infinity.  (A +infinity logit makes every score of its beam NaN.)
  *   logits     device float32 (MKV_F32) or fp16 (MKV_F16) [n_batch * n_beams] rows of `vocab` values,
  *              row r at logits + r * row_stride (elements, >= vocab)
  *   scores     device float32 [n_batch][n_beams]
