@@ -41,12 +41,18 @@ TreePlan tree_plan(const Shape &sh, const std::vector<SeqDesc> &seqs, int n_node
     return lo * kTreeTile;
   };
   // All workgroups are resident at once.  Where a CU has few tiles to go through, one workgroup each is
-  // best: every further split writes its rows' partial outputs, which the merge reads again, and without
-  // any split the merge's launch goes too (32 sequences of 300 fp16 tokens, 16 nodes: 19.5 us against 26.9
-  // with two a CU; 8 of 1024: 20.8 and 22.9; 2 of 4000: 20.8 and 23.4).  Over many tiles two (three of the
-  // smaller ones) hide each other's waits (8 of 8192 under KVQuant at 4 bits, 4 nodes: 71.9, 49.4 and 42.8 us
-  // with one, two and three, 16 nodes: 84.4, 59.8 and 76.8; 8 of 4000 fp16 tokens: 36.8, 34.5 and 42.4).
-  // More than fit at once are slower at every size measured.  The limits lie where the two met.
+  // best: every further split writes its rows' partial outputs, which the merge reads again (2 sequences of
+  // 4000 fp16 tokens, 16 nodes: 20.8 us against 23.4 with two a CU).  Over many tiles two, of 32 rows at most
+  // three, hide each other's waits.  With one, two and three a CU, 8 sequences of 8192 tokens: KVQuant at 4
+  // bits 71.9, 49.4 and 42.8 us at 4 nodes (16 rows), 78.3, 53.6 and 46.9 at 8 (32 rows), 84.4, 59.8 and
+  // 76.8 at 16; uniform 4-bit at 8 nodes 58.9, 42.3 and 40.5; fp16, which waits for memory alone, 53.4, 49.3
+  // and 53.0.  More than fit at once are slower at every size measured.  The limits lie where the two met:
+  // quantized tiles, with more to wait for, gain from a second workgroup earlier.
+  // Without any split the merge's launch goes too, and one a CU holds out twice as long (32 sequences, fp16,
+  // 1000 tokens: 25.8, 28.6 and 29.2 us at 4 nodes, 32.8, 36.6 and 43.1 at 16; KVQuant at 4 bits, 600 tokens,
+  // 16 nodes: 33.0, 34.7 and 43.0), but for quantized tiles under few rows, where decoding is most of the
+  // work and further splits add little to merge (600 tokens: 27.3, 25.5 and 23.7 at 4 nodes, 29.7, 28.3 and
+  // 27.0 at 8).
   p.chunk = chunk_for(kCus);
   double few = quantized ? 6 : 12;
   if (p.chunk >= longest && (!quantized || p.rows >= 64)) few *= 2;
