@@ -2,9 +2,9 @@
 //
 // A pair (a, b) becomes (a cos t - b sin t, b cos t + a sin t), t = pos * inv_freq.  The rows are read
 // once and written once; nothing else is large, so the kernel is bound by that traffic (8192 rows of 40
-// heads of 128: 168 MB in 37 us, 4.5 TB/s, where a large copy reaches 4.8; 64 rows: 3.6 us).  A thread takes
-// VEC pairs at one place of `heads` heads of one row: their angles are the same for all heads, so each
-// sine and cosine serves all of them.  The angle is formed in turns in float64 (a position past 2^16
+// heads of 128, each pass on other rows: 168 MB in 37 us a pass, 4.5 TB/s, where a large copy reaches 4.9; 64
+// rows: 3.6 us).  A thread takes VEC pairs at one place of `heads` heads of one row: their angles are the
+// same for all heads, so each sine and cosine serves all of them.  The angle is formed in turns in float64 (a position past 2^16
 // times an fp32 frequency has no bits left for its fraction in float32), its whole turns removed, and
 // the rest goes to the hardware sine and cosine, which take turns (error below 2^-20, the fp16 result's
 // half step is 2^-11 of its size).

@@ -15,19 +15,22 @@
 // maxima, waves through LDS and splits by a second launch.
 //
 // Roundings to fp16: dequantized keys and values (at most half a step, 2^-11 of the value; fp16 rows and
-// outliers are exact), uniform steps before they multiply a code (as much), and probabilities, which are
-// formed 2^kLift times too large (2^15 at most, with the reference 2^kLazy behind), so that fp16 holds
-// them to half a step down to 2^-27 of the largest and a long tail of small ones is not lost.  Everything
-// summed is float32.  Against 64 bits the outputs of quantized caches are 3e-4 to 1.1e-3 off (2-norm), of
-// fp16 ones 2.2e-4, of which their own rounding is 2.1e-4.  (Most of it is the keys' rounding; keys in two
-// fp16 parts would need half as many products again, and a second key tile in the LDS.)
+// outliers are exact), uniform middles and steps before they are put together (as much; a step below 2^-14 to
+// 2^-25, of which a code takes up to 8), and probabilities, which are formed 2^kLift times too large (2^15 at
+// most, with the reference 2^kLazy behind), so that fp16 holds them to half a step down to 2^-27 of the largest
+// and a long tail of small ones is not lost.  Everything summed is float32.  Nothing finite becomes infinite on
+// the way: uniform groups at fp16's end round towards 0, KVQuant values are held times a power of two that takes
+// their codebook to 1 (values near 0 lose as many bits as it goes past that), and results that are means of
+// finite values are held to 65504.  Against 64 bits the outputs of quantized caches are 3e-4 to 1.1e-3 off
+// (2-norm), of fp16 ones 2.2e-4, of which their own rounding is 2.1e-4.  (Most of it is the keys' rounding; keys
+// in two fp16 parts would need half as many products again, and a second key tile in the LDS.)
 //
 // What bounds it (8 sequences of 8192 tokens, 32 query and 8 kv heads of 128): few rows, the cache's bytes
-// (fp16, 1 to 16 nodes: 5.4 to 4.9 TB/s; the quantized tiles cost more than their bytes, in conversion and
+// (fp16, 1 to 16 nodes: 5.3 to 5.0 TB/s; the quantized tiles cost more than their bytes, in conversion and
 // table lookups: uniform 4-bit 2.4 TB/s, vector operations 60 % of the time; KVQuant at 4 bits 1.9, the LDS
 // half of the time); many, the matrix units, the exponentials and the LDS one after
 // another, two waves a SIMD being too few to overlap them (64 nodes: 590 to 650 TFLOP/s, where a large fp16
-// product of the library reaches 1320).
+// product of the library reaches 1330).
 
 #include <algorithm>
 
