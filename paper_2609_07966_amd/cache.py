@@ -44,7 +44,8 @@ class KVCache:
     and decode calls do no more: whoever makes their inputs or reads their outputs on another stream orders
     the two.  tree_attention, tree_accept and reorder, which go with the calls of `decoding` on the current
     stream, are ordered with the current stream where it is another one.  (That is some 27 us of host time a
-    call, for two events; none where the cache's stream is the current one.)
+    call, for two events; none where the cache's stream is the current one.  A captured call needs a cache made
+    with a stream of its own: the default stream cannot join a capture.)
     """
 
     def __init__(self, shape, cfgs, prompt_lens, codebooks=None, device="cuda", stream=None):
